@@ -340,6 +340,75 @@ int pd_measure_read_bandwidth(const void *dev_buf, size_t buf_bytes, size_t chun
 #define PD_INFO_KEPT_BYTES     6
 int pd_get_info(pd_ctx *ctx, int key, void *hip_stream, int64_t *value);
 
+/* ---- operators over a cache of keys and values held in 8 bits -------------------------------------------------------
+ * Independent of any pd_ctx; kernels run on the current device, on `hip_stream`, and no call synchronises, allocates or keeps
+ * anything, so that all of them can be captured into a graph.  The caller owns every buffer; pointers are DEVICE memory unless
+ * said otherwise, and `lens` is read when the kernels run.
+ *
+ * The cache.  Per request and key head, tokens lie in blocks of PD_BYTE_BLOCK.  A whole block is held as signed codes of 8 bits
+ * with one fp32 scale for its keys and one for its values; the tokens behind the last whole block are halves in a tail of two
+ * slots (block b uses slot b mod 2).  A token is rounded to halves when it comes (magnitudes beyond 65504 saturate, NaN stays);
+ * when its block is whole, scale = fp32(largest magnitude / 127), code = value / scale to the nearest whole number, ties to
+ * even, and the token stands for code * scale from then on: at most half a scale from what came, plus the rounding to halves.
+ * What a cache holds does not depend on the pieces in which its tokens came.  A NaN makes the scale of its block NaN, and with
+ * it every key (or value) of the block.  All arrays are contiguous, in the order written.  Whoever makes the contents in another way keeps codes
+ * within [-127, 127]. */
+#define PD_BYTE_BLOCK 64
+#define PD_TYPE_F32  0
+#define PD_TYPE_BF16 1
+#define PD_TYPE_F16  2
+typedef struct {
+  int8_t *k;                  /* [n_req][n_kv_head][n_block][64][head_dim]                                   */
+  int8_t *v;                  /* [n_req][n_kv_head][n_block][head_dim][64]                                   */
+  float *k_scale, *v_scale;   /* [n_req][n_kv_head][n_block]                                                 */
+  void *k_tail;               /* half [n_req][n_kv_head][2][64][head_dim]                                    */
+  void *v_tail;               /* half [n_req][n_kv_head][2][head_dim][64]                                    */
+  int32_t n_req, n_kv_head, head_dim, n_block;   /* head_dim 32, 64, 96 or 128; codes and tails 16-byte aligned */
+} pd_byte_cache;
+
+/* Stores new tokens of every request behind the ones that it holds.
+ *   k, v       keys and values of one of the PD_TYPE_* types: element (request, token, head, dim) of k at
+ *              k[request * k_strides[0] + token * k_strides[1] + head * k_strides[2] + dim]; strides (HOST arrays) in elements
+ *   n_new      most new tokens of a request, at least 0
+ *   counts     int32 [n_req] or NULL: new tokens of each request (NULL: n_new of every one); the others are padding, not read
+ *   lens       int32 [n_req]: tokens that each request holds WITH the new ones
+ * A request whose numbers do not fit (count outside [1, n_new], fewer tokens than new ones, more than n_block blocks hold) is
+ * left as it is.  Calls for one cache go in stream order. */
+int pd_byte_append(const pd_byte_cache *cache, const void *k, const void *v, int type, const int64_t *k_strides,
+                   const int64_t *v_strides, int n_new, const int32_t *counts, const int32_t *lens, void *hip_stream);
+
+/* Tokens first[r] .. first[r] + n_tok - 1 of every request as the values that they stand for, rounded to `type` (a half beyond
+ * its range is infinite); zeros where a request holds none.
+ *   first      int32 [n_req] or NULL (0); negative numbers count as 0
+ *   out_k, out_v   [n_req][n_tok][n_kv_head][head_dim], 16-byte aligned */
+int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, int n_tok, const int32_t *lens, void *out_k, void *out_v,
+                 int type, void *hip_stream);
+
+/* Attention of n_row query rows of every request over its cache: out = sum_j p_j v_j / sum_j p_j with p_j = exp(scale q.k_j)
+ * over the tokens j that the row sees: j < lens[request], j < its limit, tag of j at most its own (what is not given does not
+ * restrict; this is the dependency rule of Section 3.2 with subsequence numbers for tags and 0 for the input's tokens, and a
+ * causal piece of a prompt with limits).  A row that sees nothing gets zeros.  Query head h reads key head
+ * h / (n_head / n_kv_head).
+ *   q          [n_req][n_row][n_head][head_dim] of one of the PD_TYPE_* types, by strides as in pd_byte_append (HOST array of
+ *              three: request, row, head)
+ *   lens       int32 [n_req]; beyond what the cache holds counts as full, negative as 0
+ *   row_limit  int32 [n_req][n_row] or NULL
+ *   key_tag    uint16 [n_req][n_block * 64] and row_tag int32 [n_req][n_row], both or neither; key_tag 16-byte aligned
+ *   max_len    HOST number that no entry of lens exceeds, for the shape of the launch (0: what the cache has room for); tokens
+ *              beyond it may be left out
+ *   out        [n_req][n_row][n_head][head_dim], type of q, 16-byte aligned, not overlapping q
+ *   out_lse    fp32 [n_req][n_row][n_head] or NULL: log(sum_j exp(scale q.k_j)), -infinity for a row that sees nothing
+ *   workspace  at least pd_byte_attention_workspace_bytes (same arguments; 0: they are invalid), 16-byte aligned; it holds
+ *              nothing between calls, and calls that may overlap need one each
+ * Codes enter the products exactly; 16-bit queries too, but for parts 2^24 times smaller than the row's largest.  Probabilities are
+ * rounded to halves (relative 2^-12; fp32 and half queries: pairs of halves, 2^-23), sums and the running maximum are fp32.  Infinities and NaN
+ * in tokens that a row does not see do not reach it, save that a NaN reaches every row that sees any token of its block. */
+size_t pd_byte_attention_workspace_bytes(const pd_byte_cache *cache, int n_head, int n_row, int max_len);
+int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const int64_t *q_strides, int n_head, int n_row,
+                      const int32_t *lens, const int32_t *row_limit, const uint16_t *key_tag, const int32_t *row_tag,
+                      float scale, int max_len, void *out, float *out_lse, void *workspace, size_t workspace_bytes,
+                      void *hip_stream);
+
 /* Message for the last error on this thread (static storage, never NULL). */
 const char *pd_last_error(void);
 

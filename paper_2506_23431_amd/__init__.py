@@ -7,3 +7,4 @@ not been built (there is no CPU fallback).
 """
 
 from .binding import PipelinedDecoder, load, PdError  # noqa: F401
+from .byte_cache import ByteCache  # noqa: F401

@@ -23,7 +23,8 @@ PD_INFO_KEPT_BYTES = 6
 
 EXPORTS = ["pd_workspace_bytes", "pd_create", "pd_destroy", "pd_prefill_context", "pd_decode_step",
            "pd_generate", "pd_generate_static", "pd_decode_steps", "pd_reset_decode", "pd_set_option", "pd_profile_read",
-           "pd_measure_read_bandwidth", "pd_get_info", "pd_last_error", "pd_encdec_workspace_bytes", "pd_encdec_create", "pd_teacher_forced"]
+           "pd_measure_read_bandwidth", "pd_get_info", "pd_last_error", "pd_encdec_workspace_bytes", "pd_encdec_create", "pd_teacher_forced",
+           "pd_byte_append", "pd_byte_read", "pd_byte_attention_workspace_bytes", "pd_byte_attention"]
 
 
 class PdError(RuntimeError):
@@ -50,6 +51,11 @@ class PdEncDecConfig(C.Structure):
                                          "vocab", "rel_buckets", "rel_max_distance")] + \
                [("norm_eps", C.c_float)] + \
                [(n, C.c_int32) for n in ("bos_id", "eos_id", "max_batch", "max_ctx", "max_sub", "max_sub_tokens")]
+
+
+class PdByteCache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail")] + \
+               [(n, C.c_int32) for n in ("n_req", "n_kv_head", "head_dim", "n_block")]
 
 
 _ENCDEC_GLOBAL = ("tok_emb", "lm_head", "enc_rel_bias", "dec_rel_bias", "enc_final_norm_g", "dec_final_norm_g")
@@ -98,6 +104,13 @@ def load():
     lib.pd_encdec_workspace_bytes.argtypes = [C.POINTER(PdEncDecConfig)]
     lib.pd_encdec_create.argtypes = [C.POINTER(PdEncDecConfig), C.POINTER(PdEncDecWeights), vp, C.c_size_t, vp,
                                      C.POINTER(vp)]
+    cache, i64p, sz = C.POINTER(PdByteCache), C.POINTER(C.c_int64), C.c_size_t
+    lib.pd_byte_append.argtypes = [cache, vp, vp, C.c_int, i64p, i64p, C.c_int, vp, vp, vp]
+    lib.pd_byte_read.argtypes = [cache, vp, C.c_int, vp, vp, vp, C.c_int, vp]
+    lib.pd_byte_attention_workspace_bytes.restype = sz
+    lib.pd_byte_attention_workspace_bytes.argtypes = [cache, C.c_int, C.c_int, C.c_int]
+    lib.pd_byte_attention.argtypes = [cache, vp, C.c_int, i64p, C.c_int, C.c_int, vp, vp, vp, vp, C.c_float, C.c_int, vp, vp,
+                                      vp, sz, vp]
     for name in EXPORTS:
         getattr(lib, name)
     _lib = lib

@@ -1,0 +1,668 @@
+// A cache of keys and values in 8 bits: storing tokens, reading them back, attention over them.
+//
+// Per request and key head, tokens lie in blocks of 64.  A whole block holds signed codes of 8 bits and one fp32 scale for its
+// keys, one for its values; the tokens behind the last whole block are halves in a tail of two slots (block b: slot b & 1):
+//   k [block][64][hd], v [block][hd][64] int8;  k_tail [2][64][hd], v_tail [2][hd][64] half;  scales [block] fp32.
+// 64 tokens, and values by dims, because a lane of the 16x16x32 matrix instruction then loads 16 bytes that are operands as
+// they lie: 16 dims of a key are two contraction steps of the scores, 16 keys of a value's dim two of the outputs (any order of
+// the contraction is right that both operands share).
+#include "byte_cache.h"
+
+#include <algorithm>
+#include <type_traits>
+
+// ---------------------------------------------------------------------------
+// store
+// ---------------------------------------------------------------------------
+struct StoreArgs {
+  ByteCache c;
+  const void *src[2];                 // new keys, new values
+  int64_t s_req[2], s_tok[2], s_head[2];
+  const int32_t *counts, *lens;
+  int n_new, span;                    // most new tokens; blocks that they can touch
+};
+
+// NaN stays, everything else beyond the halves saturates
+__device__ __forceinline__ f16_t to_half(float x) { return x != x ? (f16_t)x : f32_to_f16_sat(x); }
+
+// The whole number nearest to x / s, ties to even, exactly: the product with the reciprocal is at most one off, and the
+// remainder, a whole multiple of the scale's last bit below 2^24 of them, is computed without rounding.
+__device__ __forceinline__ int code_of(float x, float s, float inv) {
+  float q = rintf(x * inv);
+  const float r = fmaf(-q, s, x), h = 0.5f * s;
+  const bool odd = ((int)q & 1) != 0;
+  q += (r > h || (r == h && odd)) ? 1.f : (r < -h || (r == -h && odd)) ? -1.f : 0.f;
+  return (int)fminf(fmaxf(q, -127.f), 127.f);
+}
+
+// One work-group per (request, head, touched block, keys or values): the block's tokens go to LDS as halves, the old ones from
+// the tail, the new ones from the caller; a whole block leaves as codes, a block that is not yet whole as halves of its new
+// tokens.  Bound by the bytes.
+template <typename T, int HD, bool WIDE>
+__global__ __launch_bounds__(256) void k_byte_store(StoreArgs a) {
+  constexpr int P = HD + 8;                              // halves per token row in LDS (16-byte rows)
+  __shared__ f16_t tile[BYTE_BLOCK * P];
+  __shared__ uint32_t sm_top[4];
+  const int tid = threadIdx.x;
+  const int kind = blockIdx.x & 1, u = blockIdx.x >> 1;
+  const int i0 = u % a.span, rh = u / a.span, h = rh % a.c.n_kv_head, req = rh / a.c.n_kv_head;
+  const int count = a.counts ? a.counts[req] : a.n_new, len = a.lens[req], before = len - count;
+  if (count <= 0 || count > a.n_new || before < 0 || (int64_t)len > (int64_t)a.c.n_block * BYTE_BLOCK) return;
+  const int first = before / BYTE_BLOCK, last = (len - 1) / BYTE_BLOCK;      // touched blocks
+  const bool part = len % BYTE_BLOCK != 0;               // the last one stays in the tail
+  // A last block with the first one's slot in the tail is stored by the work-group that has read that slot.
+  const bool shared_slot = part && last > first && ((last - first) & 1) == 0;
+  if (first + i0 > last || (shared_slot && i0 > 0 && first + i0 == last)) return;
+  const size_t rhz = (size_t)req * a.c.n_kv_head + h;
+  const T *src = (const T *)(kind ? a.src[1] : a.src[0]) + req * a.s_req[kind] + h * a.s_head[kind];
+  const int64_t s_tok = a.s_tok[kind];
+  f16_t *tail0 = (f16_t *)(kind ? a.c.v_tail : a.c.k_tail) + rhz * 2 * BYTE_BLOCK * HD;
+  for (int pass = 0; pass < (i0 == 0 && shared_slot ? 2 : 1); ++pass) {
+    const int b = pass ? last : first + i0, t0 = b * BYTE_BLOCK;
+    const bool whole = t0 + BYTE_BLOCK <= len;
+    const int n_old = min(max(before - t0, 0), BYTE_BLOCK), n_all = min(len - t0, BYTE_BLOCK);
+    f16_t *tail = tail0 + (size_t)(b & 1) * BYTE_BLOCK * HD;
+    if (pass) __syncthreads();
+    // new tokens, 8 dims at a time
+    uint32_t top = 0;
+    for (int e = tid; e < BYTE_BLOCK * (HD / 8); e += 256) {
+      const int t = e / (HD / 8), d = e % (HD / 8) * 8;
+      if (t < n_old || t >= n_all) continue;
+      const T *p = src + (int64_t)(t0 + t - before) * s_tok + d;
+      float x[8];
+      load8<T, WIDE>(p, x);
+      union { f16_t h[8]; uint4 q; } y;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        y.h[j] = to_half(x[j]);
+        top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y.h[j]) & 0x7fff));
+      }
+      if (!whole && !kind) *(uint4 *)(tail + (size_t)t * HD + d) = y.q;
+      *(uint4 *)&tile[t * P + d] = y.q;
+    }
+    if (!whole) {
+      if (kind) {                                        // values lie by dims: 2 bytes per token and dim
+        __syncthreads();
+        const int n = n_all - n_old;
+        for (int e = tid; e < n * HD; e += 256) {
+          const int d = e / n, t = n_old + e % n;
+          tail[(size_t)d * BYTE_BLOCK + t] = tile[t * P + d];
+        }
+      }
+      continue;
+    }
+    // ... and the ones that were in the tail
+    for (int e = tid; e < n_old * HD; e += 256) {
+      int t, d;
+      if (kind) { d = e / n_old; t = e % n_old; } else { t = e / HD; d = e % HD; }
+      const f16_t y = kind ? tail[(size_t)d * BYTE_BLOCK + t] : tail[(size_t)t * HD + d];
+      top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y) & 0x7fff));
+      tile[t * P + d] = y;
+    }
+    // the largest magnitude by its bits, where NaN is above everything: then the scale is NaN, and so is the block
+    for (int m = 32; m; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+    if ((tid & 63) == 0) sm_top[tid >> 6] = top;
+    __syncthreads();
+    top = max(max(sm_top[0], sm_top[1]), max(sm_top[2], sm_top[3]));
+    const float scale = __fdiv_rn((float)__builtin_bit_cast(f16_t, (uint16_t)top), 127.f);
+    const float inv = scale > 0.f ? 1.f / scale : 0.f;
+    if (tid == 0) (kind ? a.c.v_scale : a.c.k_scale)[rhz * a.c.n_block + b] = scale;
+    int8_t *dst = (kind ? a.c.v : a.c.k) + (rhz * a.c.n_block + b) * BYTE_BLOCK * HD;
+    for (int e = tid; e < BYTE_BLOCK * HD / 16; e += 256) {
+      union { int8_t c[16]; uint4 q; } y;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int o = e * 16 + j;
+        const f16_t x = kind ? tile[(o % BYTE_BLOCK) * P + o / BYTE_BLOCK] : tile[o / HD * P + o % HD];
+        y.c[j] = inv > 0.f ? (int8_t)code_of((float)x, scale, inv) : (int8_t)0;
+      }
+      ((uint4 *)dst)[e] = y.q;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// read
+// ---------------------------------------------------------------------------
+struct ReadArgs {
+  ByteCache c;
+  void *out[2];                       // [req][n_tok][head][hd]
+  const int32_t *first, *lens;
+  int n_tok, span;
+};
+
+// One work-group per (request, head, block that the range can touch, keys or values).
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_byte_read(ReadArgs a) {
+  constexpr int P = HD + 8;
+  __shared__ f16_t tile[BYTE_BLOCK * P];                 // codes are whole numbers up to 127: halves hold them
+  const int tid = threadIdx.x;
+  const int kind = blockIdx.x & 1, u = blockIdx.x >> 1;
+  const int i0 = u % a.span, rh = u / a.span, h = rh % a.c.n_kv_head, req = rh / a.c.n_kv_head;
+  const int64_t cap = (int64_t)a.c.n_block * BYTE_BLOCK;
+  const int len = (int)min((int64_t)max(a.lens[req], 0), cap);
+  const int from = a.first ? max(a.first[req], 0) : 0;
+  const int64_t b = from / BYTE_BLOCK + i0, t0 = b * BYTE_BLOCK;
+  if (t0 >= (int64_t)from + a.n_tok) return;
+  const size_t rhz = (size_t)req * a.c.n_kv_head + h;
+  const bool whole = t0 + BYTE_BLOCK <= len;
+  const int n = (int)min(max((int64_t)len - t0, (int64_t)0), (int64_t)BYTE_BLOCK);
+  float scale = 1.f;
+  if (whole) {
+    scale = (kind ? a.c.v_scale : a.c.k_scale)[rhz * a.c.n_block + b];
+    const uint4 *src = (const uint4 *)((kind ? a.c.v : a.c.k) + (rhz * a.c.n_block + b) * BYTE_BLOCK * HD);
+    for (int e = tid; e < BYTE_BLOCK * HD / 16; e += 256) {
+      union { uint4 q; int8_t c[16]; } x;
+      x.q = src[e];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int o = e * 16 + j;
+        tile[kind ? (o % BYTE_BLOCK) * P + o / BYTE_BLOCK : o / HD * P + o % HD] = (f16_t)(float)x.c[j];
+      }
+    }
+  } else if (n > 0) {
+    const f16_t *src = (const f16_t *)(kind ? a.c.v_tail : a.c.k_tail) + (rhz * 2 + (b & 1)) * BYTE_BLOCK * HD;
+    for (int e = tid; e < n * HD; e += 256) {
+      int t, d;
+      if (kind) { d = e / n; t = e % n; } else { t = e / HD; d = e % HD; }
+      tile[t * P + d] = kind ? src[(size_t)d * BYTE_BLOCK + t] : src[(size_t)t * HD + d];
+    }
+  }
+  __syncthreads();
+  T *out = (T *)(kind ? a.out[1] : a.out[0]);
+  for (int e = tid; e < BYTE_BLOCK * (HD / 8); e += 256) {
+    const int t = e / (HD / 8), d = e % (HD / 8) * 8;
+    const int64_t at = t0 + t - from;
+    if (at < 0 || at >= a.n_tok) continue;
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = t < n ? (float)tile[t * P + d + j] * scale : 0.f;
+    store8(out + (((size_t)req * a.n_tok + at) * a.c.n_kv_head + h) * HD + d, y);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------
+struct ByteAttnArgs {
+  ByteCache c;
+  const void *q;                      // [req][row][head][hd] by strides
+  int64_t q_req, q_row, q_head;
+  const int32_t *lens, *row_limit, *row_tag;
+  const uint16_t *key_tag;            // [req][n_block * 64]
+  void *out;                          // [req][row][head][hd]
+  float *lse;                         // [req][row][head] or NULL
+  float *part;
+  int n_row, group, nqg, nsplit, nblk;     // group: query heads per key head; nqg: groups of 16 (row, query head) columns
+  float scale_log2;
+  int wide_q;
+};
+
+// Four codes as four halves, exactly: a byte with its sign bit turned is code + 128, under 0x64 it is the half 1024 + 128 +
+// code, and the subtraction leaves the code (conversion by instruction takes twice as many).
+__device__ __forceinline__ void halves_of(uint32_t codes, uint32_t &lo, uint32_t &hi) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t u = codes ^ 0x80808080u;
+  const f16x2 off = {(f16_t)1152.f, (f16_t)1152.f};
+  const uint32_t a = __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u), b = __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u);
+  lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, a) - off);
+  hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, b) - off);
+}
+__device__ __forceinline__ Frag frag_of(uint32_t c0, uint32_t c1) {
+  Frag f;
+  halves_of(c0, f.u.x, f.u.y);
+  halves_of(c1, f.u.z, f.u.w);
+  return f;
+}
+
+// Probabilities are held as 2^15 p: halves then keep their full precision down to 2^-29 instead of 2^-14, and the sums carry
+// the same factor.
+constexpr float P_BITS = 15.f;
+
+// grid: (split, group of 16 columns, key head, request); NW waves.  The blocks of 64 tokens of a (request, key head) are dealt
+// round-robin to the waves of its splits.  A column is one query vector (row, query head of the key head's group).  Scores come
+// out of the matrix instruction with a lane holding 16 tokens of one column, in the order in which it is their operand for the
+// outputs: token 16 g + 8 s + e of the block is contraction slot (g, e) of step s.  Codes become halves in registers, exactly;
+// a block's key scale multiplies its scores, its value scale the sum over the block, which is added up in fp32.
+// QP, PP: queries, probabilities as pairs of halves (22 bits).  fp32 queries need both; half outputs are rounded as finely as
+// single probabilities would be, so that theirs are pairs too (error of the whole 1.3 times the output's rounding without).
+template <typename T, int HD, bool QP, bool PP, int NW>
+__global__ __launch_bounds__(64 * NW) void k_byte_attn(ByteAttnArgs a) {
+  constexpr int NS = HD / 32, NT = HD / 16;              // contraction steps of the scores, 16-dim tiles of the outputs
+  constexpr int KW = HD / 64;                            // 16-byte loads per key and lane (8 bytes more where a step is left)
+  constexpr int PSTR = HD + 2;
+  __shared__ uint4 sm_q[(QP ? 2 : 1) * NS][64];
+  __shared__ float sm_qf[16];
+  __shared__ uint32_t sm_top[16][16];
+  __shared__ float sm_m[NW][16], sm_l[NW][16];
+  __shared__ floatx4 sm_o[NW][NT][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  int u = blockIdx.x;
+  const int split = u % a.nsplit; u /= a.nsplit;
+  const int qg = u % a.nqg; u /= a.nqg;
+  const int h = u % a.c.n_kv_head, req = u / a.c.n_kv_head;
+  const int n_cols = a.n_row * a.group;
+  const size_t rhz = (size_t)req * a.c.n_kv_head + h;
+
+  // ---- the queries of the 16 columns, in operand order, divided by a power of two that brings a row's largest below 512 ----
+  {
+    constexpr int DP = HD / 16;                          // dims per (column, part)
+    const int part = threadIdx.x >> 4;                   // 16 parts of a column; NW = 4: one each
+    for (int pt = part; pt < 16; pt += NW * 4) {
+      const int col = qg * 16 + n;
+      float x[DP];
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < DP; ++j) x[j] = 0.f;
+      if (col < n_cols) {
+        const int row = col / a.group, hq = h * a.group + col % a.group;
+        const T *p = (const T *)a.q + req * a.q_req + row * a.q_row + hq * a.q_head + pt * DP;
+#pragma unroll
+        for (int j = 0; j < DP; ++j) x[j] = ld_f32(p, j);
+      }
+#pragma unroll
+      for (int j = 0; j < DP; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+      sm_top[pt][n] = top;
+    }
+    __syncthreads();
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) top = max(top, sm_top[j][n]);
+    // exponent of the largest, held where both powers are normal numbers; not a number, infinite: as it is
+    const int ex = top >= 0x7f800000u ? 8 : max((int)(top >> 23) - 127, -100);
+    const float down = __uint_as_float((uint32_t)(127 + 8 - ex) << 23);
+    if (threadIdx.x < 16) sm_qf[n] = __uint_as_float((uint32_t)(127 - 8 + ex) << 23) * a.scale_log2;
+    for (int pt = part; pt < 16; pt += NW * 4) {
+      const int col = qg * 16 + n;
+      const int row = col / a.group, hq = h * a.group + col % a.group;
+      const T *p = (const T *)a.q + req * a.q_req + row * a.q_row + hq * a.q_head + pt * DP;
+#pragma unroll
+      for (int j = 0; j < DP; ++j) {
+        const int d = pt * DP + j;
+        const float x = col < n_cols ? ld_f32(p, j) * down : 0.f;
+        const f16_t hi = (f16_t)x;
+        // dim -> (step, group, element): 16 dims of a 16-byte load are 8 of two steps
+        int step, gg;
+        if (d < KW * 64) { step = (d >> 6) * 2 + ((d >> 3) & 1); gg = (d & 63) >> 4; }
+        else { step = 2 * KW; gg = (d & 31) >> 3; }
+        ((f16_t *)&sm_q[step][gg * 16 + n])[d & 7] = hi;
+        if (QP) ((f16_t *)&sm_q[(QP ? NS : 0) + step][gg * 16 + n])[d & 7] = (f16_t)(x - (float)hi);
+      }
+    }
+  }
+  // ---- what the columns see ----
+  const int cap = a.c.n_block * BYTE_BLOCK;
+  const int n_keys = min(max(a.lens[req], 0), cap);
+  const int col = qg * 16 + n, row = min(col, n_cols - 1) / a.group;
+  int lim = col < n_cols ? n_keys : 0;
+  if (a.row_limit) lim = min(lim, max(a.row_limit[(size_t)req * a.n_row + row], 0));
+  const int tag = a.key_tag ? a.row_tag[(size_t)req * a.n_row + row] : 0;
+  const int reach = __builtin_amdgcn_readfirstlane(fold_row(lim, Max()));
+  const int lim_all = __builtin_amdgcn_readfirstlane(fold_row(col < n_cols ? lim : 0x7fffffff, Min()));
+  const int whole = n_keys / BYTE_BLOCK;                 // blocks of codes; the next one is the tail
+  const int end = min((reach + BYTE_BLOCK - 1) / BYTE_BLOCK, a.nblk);
+  __syncthreads();
+  const float qf = sm_qf[n];
+
+  const int8_t *K = a.c.k + rhz * a.c.n_block * BYTE_BLOCK * HD, *V = a.c.v + rhz * a.c.n_block * BYTE_BLOCK * HD;
+  float m_run = -INFINITY, l_run = 0.f;
+  floatx4 o[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  for (int kb = split * NW + wave; kb < end; kb += NW * a.nsplit) {
+    const bool sealed = kb < whole;
+    Frag vt[NT][2];
+    floatx4 s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    float kf = qf, vf = 1.f;
+    const int key_m = 16 * (n >> 2) + (n & 3);           // key of operand row n of score tile 0 (tile t: + 4 t)
+    if (sealed) {
+      const int8_t *kp = K + (size_t)kb * BYTE_BLOCK * HD, *vp = V + (size_t)kb * BYTE_BLOCK * HD;
+      kf *= a.c.k_scale[rhz * a.c.n_block + kb];
+      vf = a.c.v_scale[rhz * a.c.n_block + kb];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int8_t *kr = kp + (key_m + 4 * t) * HD;
+#pragma unroll
+        for (int c = 0; c < NS; ++c) {
+          uint2 x;
+          if (c < 2 * KW) x = *(const uint2 *)(kr + (c >> 1) * 64 + g * 16 + (c & 1) * 8);
+          else x = *(const uint2 *)(kr + KW * 64 + g * 8);
+          const Frag f = frag_of(x.x, x.y);
+          Frag q;
+          q.u = sm_q[c][lane];
+          s[t] = mfma16h(f, q, s[t]);
+          if (QP) { q.u = sm_q[(QP ? NS : 0) + c][lane]; s[t] = mfma16h(f, q, s[t]); }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const uint4 x = *(const uint4 *)(vp + (i * 16 + n) * BYTE_BLOCK + g * 16);
+        vt[i][0] = frag_of(x.x, x.y);
+        vt[i][1] = frag_of(x.z, x.w);
+      }
+    } else {
+      const f16_t *kp = (const f16_t *)a.c.k_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD;
+      const f16_t *vp = (const f16_t *)a.c.v_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const f16_t *kr = kp + (key_m + 4 * t) * HD;
+#pragma unroll
+        for (int c = 0; c < NS; ++c) {
+          Frag f, q;
+          f.u = *(const uint4 *)(kr + (c < 2 * KW ? (c >> 1) * 64 + g * 16 + (c & 1) * 8 : KW * 64 + g * 8));
+          q.u = sm_q[c][lane];
+          s[t] = mfma16h(f, q, s[t]);
+          if (QP) { q.u = sm_q[(QP ? NS : 0) + c][lane]; s[t] = mfma16h(f, q, s[t]); }
+        }
+      }
+      // slots without a token hold anything: zeros instead, so that no product with a zero is NaN
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          vt[i][st].u = *(const uint4 *)(vp + (i * 16 + n) * BYTE_BLOCK + g * 16 + st * 8);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (kb * BYTE_BLOCK + 16 * g + 8 * st + e >= n_keys) vt[i][st].hh[e] = (f16_t)0.f;
+        }
+    }
+    // lane (n, g), element e  <->  token kb * 64 + 16 g + e
+    float sv[16];
+    const int key0 = kb * BYTE_BLOCK + 16 * g;
+    if (!a.key_tag && kb * BYTE_BLOCK + BYTE_BLOCK <= lim_all) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sv[e] = s[e >> 2][e & 3] * kf;
+    } else {
+      union { uint4 u[2]; uint16_t s[16]; } tg;
+      if (a.key_tag) {
+        const uint4 *tp = (const uint4 *)(a.key_tag + (size_t)req * cap + key0);
+        tg.u[0] = tp[0]; tg.u[1] = tp[1];
+      } else {
+        tg.u[0] = tg.u[1] = make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sv[e] = ((key0 + e < lim) & ((int)tg.s[e] <= tag)) ? s[e >> 2][e & 3] * kf : -INFINITY;
+    }
+    float mloc = sv[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mloc = fmaxf(mloc, sv[e]);
+    mloc = fold32(fold16(mloc, Max()), Max());
+    const float m_new = fmaxf(m_run, mloc), m_ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_ref);
+    Frag ph[2], pl[2];
+    float psum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float p = __builtin_amdgcn_exp2f(sv[e] - (m_ref - P_BITS));
+      psum += p;
+      ph[e >> 3].hh[e & 7] = (f16_t)p;
+      if (PP) pl[e >> 3].hh[e & 7] = (f16_t)(p - (float)ph[e >> 3].hh[e & 7]);
+    }
+    l_run = l_run * alpha + psum;
+    m_run = m_new;
+    if (__any(alpha != 1.f))
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[i] *= alpha;
+    // a column that sees nothing of the block takes nothing from it, whatever its scale is
+    const bool some = fold32(fold16(psum, Add()), Add()) != 0.f;
+    const float vfs = some ? vf : 0.f;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      floatx4 t = mfma16h(vt[i][0], ph[0], floatx4{0.f, 0.f, 0.f, 0.f});
+      t = mfma16h(vt[i][1], ph[1], t);
+      if (PP) { t = mfma16h(vt[i][0], pl[0], t); t = mfma16h(vt[i][1], pl[1], t); }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] = sealed || some ? fmaf(t[e], vfs, o[i][e]) : o[i][e];
+    }
+  }
+  l_run = fold32(fold16(l_run, Add()), Add());
+
+  // ---- the waves' states become one ----
+  if (g == 0) { sm_m[wave][n] = m_run; sm_l[wave][n] = l_run; }
+#pragma unroll
+  for (int i = 0; i < NT; ++i) sm_o[wave][i][lane] = o[i];
+  __syncthreads();
+  float fw[NW], M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) { fw[w] = sm_m[w][n]; M = fmaxf(M, fw[w]); }
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    // (a wave whose keys are all NaN has no maximum but a sum)
+    fw[w] = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fw[w] - M);
+    L += fw[w] * sm_l[w][n];
+  }
+  const size_t unit = rhz * a.nqg + qg;
+  if (a.nsplit > 1) {
+    float *pp = a.part + (unit * a.nsplit + split) * (size_t)(PSTR * 16);
+    if (wave == 0 && g == 0) { pp[n] = M; pp[16 + n] = L; }
+    for (int i = wave; i < NT; i += NW) {
+      floatx4 y = fw[0] * sm_o[0][i][lane];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) y += fw[w] * sm_o[w][i][lane];
+      *(floatx4 *)(pp + 32 + ((i * 4 + g) * 16 + n) * 4) = y;
+    }
+    return;
+  }
+  if (col >= n_cols) return;
+  const size_t at = ((size_t)req * a.n_row + row) * a.c.n_kv_head * a.group + h * a.group + col % a.group;
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  if (a.lse && wave == 0 && g == 0) a.lse[at] = (M + (__builtin_amdgcn_logf(L) - P_BITS)) * 0.6931471805599453f;
+  for (int i = wave; i < NT; i += NW) {
+    floatx4 y = fw[0] * sm_o[0][i][lane];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) y += fw[w] * sm_o[w][i][lane];
+    y *= inv;
+    store4((T *)a.out + at * HD + i * 16 + 4 * g, y);
+  }
+}
+
+// The splits of a unit become one: a block per (unit, 16-dim tile), wave w takes the splits w, w + 4, ...
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_byte_merge(ByteAttnArgs a) {
+  constexpr int PSTR = HD + 2, NT = HD / 16;
+  __shared__ float sm_m[4][64], sm_l[4][64];
+  __shared__ floatx4 sm_o[4][64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int i = blockIdx.x % NT;
+  const size_t unit = blockIdx.x / NT;
+  const int qg = unit % a.nqg, h = unit / a.nqg % a.c.n_kv_head, req = unit / a.nqg / a.c.n_kv_head;
+  const float *pb = a.part + unit * a.nsplit * (size_t)(PSTR * 16);
+  float M = -INFINITY, L = 0.f;
+  floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int s = wave; s < a.nsplit; s += 4) {
+    const float *p = pb + (size_t)s * (PSTR * 16);
+    const float m = p[n], l = p[16 + n];
+    const floatx4 x = *(const floatx4 *)(p + 32 + ((i * 4 + g) * 16 + n) * 4);
+    const float Mn = fmaxf(M, m), ref = Mn == -INFINITY ? 0.f : Mn;
+    const float fo = M == -INFINITY && Mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - ref);
+    const float fx = m == -INFINITY && Mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - ref);
+    L = L * fo + l * fx;
+    o = o * fo + x * fx;
+    M = Mn;
+  }
+  sm_m[wave][lane] = M; sm_l[wave][lane] = L; sm_o[wave][lane] = o;
+  __syncthreads();
+  const int col = qg * 16 + n;
+  if (wave != 0 || col >= a.n_row * a.group) return;
+  M = fmaxf(fmaxf(sm_m[0][lane], sm_m[1][lane]), fmaxf(sm_m[2][lane], sm_m[3][lane]));
+  L = 0.f; o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm_m[w][lane] - M);
+    L += f * sm_l[w][lane];
+    o += f * sm_o[w][lane];
+  }
+  const size_t at = ((size_t)req * a.n_row + col / a.group) * a.c.n_kv_head * a.group + h * a.group + col % a.group;
+  if (a.lse && i == 0 && g == 0) a.lse[at] = (M + (__builtin_amdgcn_logf(L) - P_BITS)) * 0.6931471805599453f;
+  o *= L == 0.f ? 0.f : 1.f / L;
+  store4((T *)a.out + at * HD + i * 16 + 4 * g, o);
+}
+
+// ---------------------------------------------------------------------------
+// entry points
+// ---------------------------------------------------------------------------
+static int check_cache(const pd_byte_cache *c) {
+  PD_REQUIRE(c, PD_EINVAL, "cache is NULL");
+  PD_REQUIRE(c->n_req >= 1 && c->n_kv_head >= 1 && c->n_block >= 1, PD_EINVAL,
+             "a byte cache has at least one request, head and block (got %d, %d, %d)", c->n_req, c->n_kv_head, c->n_block);
+  PD_REQUIRE(c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 96 || c->head_dim == 128, PD_EINVAL,
+             "head_dim must be 32, 64, 96 or 128 (got %d)", c->head_dim);
+  PD_REQUIRE(c->n_block <= (1 << 24), PD_EINVAL, "%d blocks per request: at most 2^24", c->n_block);
+  PD_REQUIRE((int64_t)c->n_req * c->n_kv_head < (1ll << 26), PD_EINVAL, "too many requests and heads (%d x %d)", c->n_req,
+             c->n_kv_head);
+  PD_REQUIRE(c->k && c->v && c->k_scale && c->v_scale && c->k_tail && c->v_tail, PD_EINVAL, "a pointer of the cache is NULL");
+  PD_REQUIRE((((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->k_tail | (uintptr_t)c->v_tail) & 15) == 0 &&
+                 (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 3) == 0,
+             PD_EINVAL, "codes and tails must be 16-byte aligned, scales 4-byte aligned");
+  return PD_OK;
+}
+
+static ByteCache view(const pd_byte_cache *c) {
+  return ByteCache{(int8_t *)c->k, (int8_t *)c->v, c->k_scale, c->v_scale, c->k_tail, c->v_tail, c->n_req, c->n_kv_head, c->n_block};
+}
+
+static int type_bytes(int type) { return type == PD_TYPE_F32 ? 4 : 2; }
+static int check_type(int type) {
+  PD_REQUIRE(type == PD_TYPE_F32 || type == PD_TYPE_BF16 || type == PD_TYPE_F16, PD_EINVAL,
+             "type must be PD_TYPE_F32, PD_TYPE_BF16 or PD_TYPE_F16 (got %d)", type);
+  return PD_OK;
+}
+static int check_grid(int64_t blocks) {
+  PD_REQUIRE(blocks < (1ll << 31), PD_EINVAL, "a launch of %lld work-groups is too large", (long long)blocks);
+  return PD_OK;
+}
+
+// F(type, head_dim) for the run-time values
+#define PD_BYTE_DIMS(T, HDV, F)                          \
+  switch (HDV) {                                         \
+    case 32: F(T, 32); break;                            \
+    case 64: F(T, 64); break;                            \
+    case 96: F(T, 96); break;                            \
+    default: F(T, 128); break;                           \
+  }
+#define PD_BYTE_TYPES(TYPE, HDV, F)                      \
+  switch (TYPE) {                                        \
+    case PD_TYPE_F32: PD_BYTE_DIMS(float, HDV, F) break; \
+    case PD_TYPE_BF16: PD_BYTE_DIMS(bf16_t, HDV, F) break; \
+    default: PD_BYTE_DIMS(f16_t, HDV, F) break;          \
+  }
+
+extern "C" int pd_byte_append(const pd_byte_cache *cache, const void *k, const void *v, int type, const int64_t *k_strides,
+                              const int64_t *v_strides, int n_new, const int32_t *counts, const int32_t *lens, void *hip_stream) {
+  int rc;
+  if ((rc = check_cache(cache)) || (rc = check_type(type))) return rc;
+  PD_REQUIRE(n_new >= 0, PD_EINVAL, "n_new must be >= 0 (got %d)", n_new);
+  if (n_new == 0) return PD_OK;
+  PD_REQUIRE(k && v && k_strides && v_strides && lens, PD_EINVAL, "NULL argument");
+  PD_REQUIRE((int64_t)n_new <= (int64_t)cache->n_block * BYTE_BLOCK, PD_EINVAL, "%d new tokens do not fit %d blocks", n_new,
+             cache->n_block);
+  const int es = type_bytes(type);
+  PD_REQUIRE((((uintptr_t)k | (uintptr_t)v) & (es - 1)) == 0, PD_EINVAL, "keys and values must be aligned to their type");
+  StoreArgs a;
+  a.c = view(cache); a.src[0] = k; a.src[1] = v; a.counts = counts; a.lens = lens; a.n_new = n_new;
+  a.span = (n_new + BYTE_BLOCK - 2) / BYTE_BLOCK + 1;
+  uint64_t bits = (uintptr_t)k | (uintptr_t)v;
+  for (int i = 0; i < 2; ++i) {
+    const int64_t *st = i ? v_strides : k_strides;
+    a.s_req[i] = st[0]; a.s_tok[i] = st[1]; a.s_head[i] = st[2];
+    bits |= (uint64_t)((st[0] | st[1] | st[2]) * es);
+  }
+  const bool wide = (bits & 15) == 0;
+  const int64_t blocks = (int64_t)cache->n_req * cache->n_kv_head * a.span * 2;
+  if ((rc = check_grid(blocks))) return rc;
+  hipStream_t s = (hipStream_t)hip_stream;
+#define PD_STORE(T, HDV)                                                                                       \
+  do {                                                                                                         \
+    if (wide) hipLaunchKernelGGL((k_byte_store<T, HDV, true>), dim3((unsigned)blocks), dim3(256), 0, s, a);    \
+    else hipLaunchKernelGGL((k_byte_store<T, HDV, false>), dim3((unsigned)blocks), dim3(256), 0, s, a);        \
+  } while (0)
+  PD_BYTE_TYPES(type, cache->head_dim, PD_STORE)
+#undef PD_STORE
+  PD_CHECK_HIP(hipGetLastError());
+  return PD_OK;
+}
+
+extern "C" int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, int n_tok, const int32_t *lens, void *out_k,
+                            void *out_v, int type, void *hip_stream) {
+  int rc;
+  if ((rc = check_cache(cache)) || (rc = check_type(type))) return rc;
+  PD_REQUIRE(n_tok >= 0, PD_EINVAL, "n_tok must be >= 0 (got %d)", n_tok);
+  if (n_tok == 0) return PD_OK;
+  PD_REQUIRE(lens && out_k && out_v, PD_EINVAL, "NULL argument");
+  PD_REQUIRE((((uintptr_t)out_k | (uintptr_t)out_v) & 15) == 0, PD_EINVAL, "outputs must be 16-byte aligned");
+  ReadArgs a;
+  a.c = view(cache); a.out[0] = out_k; a.out[1] = out_v; a.first = first; a.lens = lens; a.n_tok = n_tok;
+  a.span = first ? (n_tok - 1 + BYTE_BLOCK - 1) / BYTE_BLOCK + 1 : (n_tok + BYTE_BLOCK - 1) / BYTE_BLOCK;
+  const int64_t blocks = (int64_t)cache->n_req * cache->n_kv_head * a.span * 2;
+  if ((rc = check_grid(blocks))) return rc;
+  hipStream_t s = (hipStream_t)hip_stream;
+#define PD_READ(T, HDV) hipLaunchKernelGGL((k_byte_read<T, HDV>), dim3((unsigned)blocks), dim3(256), 0, s, a)
+  PD_BYTE_TYPES(type, cache->head_dim, PD_READ)
+#undef PD_READ
+  PD_CHECK_HIP(hipGetLastError());
+  return PD_OK;
+}
+
+struct ByteShape { int nqg, nblk, nsplit; int64_t units; };
+
+static int byte_shape(const pd_byte_cache *c, int n_head, int n_row, int max_len, ByteShape *out) {
+  PD_REQUIRE(n_head >= 1 && n_head % c->n_kv_head == 0, PD_EINVAL, "n_head = %d is no multiple of %d key heads", n_head,
+             c->n_kv_head);
+  PD_REQUIRE(n_row >= 0 && max_len >= 0, PD_EINVAL, "n_row and max_len must be >= 0 (got %d, %d)", n_row, max_len);
+  PD_REQUIRE((int64_t)n_row * (n_head / c->n_kv_head) < (1 << 30), PD_EINVAL, "too many rows and query heads (%d x %d)", n_row,
+             n_head);
+  const int64_t cap = (int64_t)c->n_block * BYTE_BLOCK;
+  const int64_t most = max_len ? std::min<int64_t>(max_len, cap) : cap;
+  out->nqg = (n_row * (n_head / c->n_kv_head) + 15) / 16;
+  out->nblk = (int)((most + BYTE_BLOCK - 1) / BYTE_BLOCK);
+  out->units = (int64_t)c->n_req * c->n_kv_head * out->nqg;
+  out->nsplit = out->units ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / out->units, out->nblk / 8)) : 1;
+  return check_grid(out->units * std::max(out->nsplit, c->head_dim / 16));
+}
+
+extern "C" size_t pd_byte_attention_workspace_bytes(const pd_byte_cache *cache, int n_head, int n_row, int max_len) {
+  ByteShape sh;
+  if (check_cache(cache) || byte_shape(cache, n_head, n_row, max_len, &sh)) return 0;
+  return sh.nsplit > 1 ? (size_t)sh.units * sh.nsplit * 16 * (cache->head_dim + 2) * sizeof(float) : 16;
+}
+
+extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const int64_t *q_strides, int n_head,
+                                 int n_row, const int32_t *lens, const int32_t *row_limit, const uint16_t *key_tag,
+                                 const int32_t *row_tag, float scale, int max_len, void *out, float *out_lse,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream) {
+  int rc;
+  ByteShape sh;
+  if ((rc = check_cache(cache)) || (rc = check_type(type)) || (rc = byte_shape(cache, n_head, n_row, max_len, &sh))) return rc;
+  if (n_row == 0) return PD_OK;
+  PD_REQUIRE(q && q_strides && lens && out, PD_EINVAL, "NULL argument");
+  PD_REQUIRE(!key_tag == !row_tag, PD_EINVAL, "key_tag and row_tag go together");
+  PD_REQUIRE(((uintptr_t)key_tag & 15) == 0, PD_EINVAL, "key_tag must be 16-byte aligned");
+  PD_REQUIRE(((uintptr_t)out & 15) == 0, PD_EINVAL, "out must be 16-byte aligned");
+  const int es = type_bytes(type);
+  PD_REQUIRE(((uintptr_t)q & (es - 1)) == 0, PD_EINVAL, "q must be aligned to its type");
+  PD_REQUIRE(scale == scale && std::abs(scale) <= 3.0e38f, PD_EINVAL, "scale must be a finite number");
+  const size_t need = pd_byte_attention_workspace_bytes(cache, n_head, n_row, max_len);
+  PD_REQUIRE(sh.nsplit == 1 || (workspace && workspace_bytes >= need), PD_ENOMEM, "workspace too small: %zu bytes given, %zu needed",
+             workspace ? workspace_bytes : (size_t)0, need);
+  PD_REQUIRE(sh.nsplit == 1 || ((uintptr_t)workspace & 15) == 0, PD_EINVAL, "workspace must be 16-byte aligned");
+  ByteAttnArgs a;
+  a.c = view(cache); a.q = q; a.q_req = q_strides[0]; a.q_row = q_strides[1]; a.q_head = q_strides[2];
+  a.lens = lens; a.row_limit = row_limit; a.key_tag = key_tag; a.row_tag = row_tag; a.out = out; a.lse = out_lse;
+  a.part = (float *)workspace; a.n_row = n_row; a.group = n_head / cache->n_kv_head;
+  a.nqg = sh.nqg; a.nsplit = sh.nsplit; a.nblk = sh.nblk; a.scale_log2 = scale * 1.4426950408889634f; a.wide_q = 0;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const unsigned grid = (unsigned)(sh.units * sh.nsplit);
+#define PD_ATTEND(T, HDV)                                                                                                \
+  do {                                                                                                                   \
+    hipLaunchKernelGGL((k_byte_attn<T, HDV, sizeof(T) == 4, !std::is_same<T, bf16_t>::value, 4>), dim3(grid), dim3(256), 0, s, a);                        \
+    if (sh.nsplit > 1)                                                                                                   \
+      hipLaunchKernelGGL((k_byte_merge<T, HDV>), dim3((unsigned)(sh.units * (HDV / 16))), dim3(256), 0, s, a);           \
+  } while (0)
+  PD_BYTE_TYPES(type, cache->head_dim, PD_ATTEND)
+#undef PD_ATTEND
+  PD_CHECK_HIP(hipGetLastError());
+  return PD_OK;
+}
