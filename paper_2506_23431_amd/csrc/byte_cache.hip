@@ -193,9 +193,8 @@ struct ByteAttnArgs {
   void *out;                          // [req][row][head][hd]
   float *lse;                         // [req][row][head] or NULL
   float *part;
-  int n_row, group, nqg, nsplit, nblk;     // group: query heads per key head; nqg: groups of 16 (row, query head) columns
+  int n_row, group, nqg, qt, nsplit, nblk; // group: query heads per key head; nqg: groups of 16 qt (row, query head) columns
   float scale_log2;
-  int wide_q;
 };
 
 // Four codes as four halves, exactly: a byte with its sign bit turned is code + 128, under 0x64 it is the half 1024 + 128 +
@@ -219,243 +218,428 @@ __device__ __forceinline__ Frag frag_of(uint32_t c0, uint32_t c1) {
 // the same factor.
 constexpr float P_BITS = 15.f;
 
-// grid: (split, group of 16 columns, key head, request); NW waves.  The blocks of 64 tokens of a (request, key head) are dealt
+// (a condition that is the same for the whole wave, as a branch of the scalar unit)
+__device__ __forceinline__ bool uniform(bool c) { return __builtin_amdgcn_readfirstlane(c ? 1 : 0) != 0; }
+__device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x); }
+
+// Codes that a launch reads once (ONCE: one tile of columns per key head) are loaded with the non-temporal hint: us per launch with
+// ordinary loads / with the hint, 4 requests x 32 heads x 5000 tokens of size 128 32.3 / 30.3, 32 x 8 x 8192 78.3 / 73.7, 16 x 8461
+// 17.7 / 17.5, 12 x 1000 of size 64 8.1 / 8.1.  Groups of columns re-read them from L2: 1 x 16 heads, 2048 rows 133 / 143.
+template <bool ONCE, typename U>
+__device__ __forceinline__ U ld_code(const int8_t *p) {
+  typedef unsigned words __attribute__((ext_vector_type(sizeof(U) / 4)));
+  return __builtin_bit_cast(U, ONCE ? __builtin_nontemporal_load((const words *)p) : *(const words *)p);
+}
+
+typedef int intx4 __attribute__((ext_vector_type(4)));
+// 16 x 16 sums of 64 products of bytes, exact
+__device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(intx4, a), __builtin_bit_cast(intx4, b), c, 0, 0, 0);
+}
+
+// grid: (split, group of 16 QT columns, key head, request); NW waves.  The blocks of 64 tokens of a (request, key head) are dealt
 // round-robin to the waves of its splits.  A column is one query vector (row, query head of the key head's group).  Scores come
 // out of the matrix instruction with a lane holding 16 tokens of one column, in the order in which it is their operand for the
-// outputs: token 16 g + 8 s + e of the block is contraction slot (g, e) of step s.  Codes become halves in registers, exactly;
-// a block's key scale multiplies its scores, its value scale the sum over the block, which is added up in fp32.
-// QP, PP: queries, probabilities as pairs of halves (22 bits).  fp32 queries need both; half outputs are rounded as finely as
-// single probabilities would be, so that theirs are pairs too (error of the whole 1.3 times the output's rounding without).
-template <typename T, int HD, bool QP, bool PP, int NW>
-__global__ __launch_bounds__(64 * NW) void k_byte_attn(ByteAttnArgs a) {
+// outputs: token 16 g + 8 s + e of the block is contraction slot (g, e) of step s.
+//  * Scores are products of bytes, exact in 32-bit integers: the keys' codes as they lie, queries as whole numbers of two bytes
+//    (bf16) or three (fp32, half), steps of the row's largest / 32512 or / 2^23.  No key is converted.
+//  * Values become halves in registers, exactly, once for QT tiles of 16 columns.
+//  * A block's key scale multiplies its scores.  The reference of the exponentials is a whole number (the running maximum
+//    rounded up), so that taking it off rounds nothing and rescaling by its change is exact.
+//  * A block's value scale multiplies its probabilities, over a power of two (vref) within 2^12 of it: the outputs add up in
+//    the matrix instruction, in units of vref, and are rescaled, exactly, in the rare case that it moves.
+//  * The sums of the probabilities are a product with ones: the same roundings as in the outputs, and no work for the vector
+//    units, which are what binds pieces of a prompt.
+// PP: probabilities as pairs of halves (22 bits): fp32 outputs need them, and half outputs are rounded as finely as single
+// probabilities would be (error of the whole 1.3 times the output's rounding without).
+template <typename T, int HD, bool PP, int QT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   constexpr int NS = HD / 32, NT = HD / 16;              // contraction steps of the scores, 16-dim tiles of the outputs
   constexpr int KW = HD / 64;                            // 16-byte loads per key and lane (8 bytes more where a step is left)
   constexpr int PSTR = HD + 2;
-  __shared__ uint4 sm_q[(QP ? 2 : 1) * NS][64];
-  __shared__ float sm_qf[16];
-  __shared__ uint32_t sm_top[16][16];
-  __shared__ float sm_m[NW][16], sm_l[NW][16];
+  constexpr int NP = sizeof(T) == 2 && !PP ? 2 : 3, NC = (HD + 63) / 64;     // bytes of a query value; contraction steps of 64
+  constexpr bool QP = sizeof(T) == 4;
+  __shared__ uint4 sm_qi[QT][NP][NC][64], sm_q[QT][(QP ? 2 : 1) * NS][64];
+  __shared__ float sm_qf[QT][2][16];
+  __shared__ uint32_t sm_top[QT][16][16];
+  __shared__ float sm_m[QT][NW][16], sm_l[QT][NW][16];
   __shared__ floatx4 sm_o[NW][NT][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  int u = blockIdx.x;
-  const int split = u % a.nsplit; u /= a.nsplit;
-  const int qg = u % a.nqg; u /= a.nqg;
-  const int h = u % a.c.n_kv_head, req = u / a.c.n_kv_head;
+  int u = blockIdx.x, split = 0, qg, unit;
+  if (a.nqg > 1) {                                       // column groups of one (request, head) on one XCD, whose cache they share
+    const int xcd = u & 7, rest = u >> 3;
+    qg = a.nqg - 1 - rest / a.nsplit % a.nqg;            // (the last rows of a causal piece have the most to do)
+    split = rest % a.nsplit;
+    unit = rest / a.nsplit / a.nqg * 8 + xcd;
+    if (unit >= a.c.n_req * a.c.n_kv_head) return;
+  } else {
+    split = u % a.nsplit; unit = u / a.nsplit; qg = 0;
+  }
+  const int h = unit % a.c.n_kv_head, req = unit / a.c.n_kv_head;
   const int n_cols = a.n_row * a.group;
-  const size_t rhz = (size_t)req * a.c.n_kv_head + h;
+  const size_t rhz = (size_t)unit;
 
-  // ---- the queries of the 16 columns, in operand order, divided by a power of two that brings a row's largest below 512 ----
+  // One block per wave is in flight while another is worked on: its keys are requested when the scores have taken the ones
+  // before, its values when the outputs have.  The first is requested before anything else is read (a wave without one asks for
+  // the last block that there is room for, and ignores it).  Scales come by vector loads, in order with the codes, so that
+  // nothing waits for all that is under way.
+  const int key_m = 16 * (n >> 2) + (n & 3);             // token of operand row n of score tile 0 (tile t: + 4 t)
+  const int8_t *K = a.c.k + rhz * a.c.n_block * BYTE_BLOCK * HD + key_m * HD;
+  const int8_t *V = a.c.v + rhz * a.c.n_block * BYTE_BLOCK * HD + n * BYTE_BLOCK + g * 16;
+  int zero;
+  asm("v_mov_b32 %0, 0" : "=v"(zero));
+  const float *KS = a.c.k_scale + rhz * a.c.n_block + zero, *VS = a.c.v_scale + rhz * a.c.n_block + zero;
+  const int stride = NW * a.nsplit;
+  int kb = split * NW + wave;
+  uint4 kw[4][KW ? KW : 1], vw[NT];
+  uint2 kn[4];
+  uint4 tg[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  float ksc, vsc;
+  const uint16_t *TG = a.key_tag ? a.key_tag + (size_t)req * a.c.n_block * BYTE_BLOCK + 16 * g : nullptr;
+  auto load_tags = [&](int b) {
+    if (TG) {
+      const uint4 *tp = (const uint4 *)(TG + (size_t)b * BYTE_BLOCK);
+      tg[0] = tp[0]; tg[1] = tp[1];
+    }
+  };
+  auto load_k = [&](int b) {
+    const int8_t *kp = K + (size_t)b * BYTE_BLOCK * HD;
+    ksc = KS[b];
+    load_tags(b);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int c = 0; c < KW; ++c) kw[t][c] = ld_code<QT == 1, uint4>(kp + 4 * t * HD + c * 64 + g * 16);
+      if (NS & 1) kn[t] = ld_code<QT == 1, uint2>(kp + 4 * t * HD + KW * 64 + g * 8);
+    }
+  };
+  auto load_v = [&](int b) {
+    const int8_t *vp = V + (size_t)b * BYTE_BLOCK * HD;
+    vsc = VS[b];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) vw[i] = ld_code<QT == 1, uint4>(vp + i * 16 * BYTE_BLOCK);
+  };
+  load_k(min(kb, a.c.n_block - 1));
+  load_v(min(kb, a.c.n_block - 1));
+  __builtin_amdgcn_sched_barrier(0);
+
+  // ---- the queries of the columns, in operand order: whole numbers of NP bytes for the codes, halves for the tail ----
   {
     constexpr int DP = HD / 16;                          // dims per (column, part)
-    const int part = threadIdx.x >> 4;                   // 16 parts of a column; NW = 4: one each
-    for (int pt = part; pt < 16; pt += NW * 4) {
-      const int col = qg * 16 + n;
-      float x[DP];
-      uint32_t top = 0;
+    constexpr int IT = (QT * 256 + NW * 64 - 1) / (NW * 64);
+    float x[IT][DP];
 #pragma unroll
-      for (int j = 0; j < DP; ++j) x[j] = 0.f;
+    for (int it = 0; it < IT; ++it) {
+      const int e = threadIdx.x + it * NW * 64, qt = e >> 8, pt = e >> 4 & 15, col = (qg * QT + qt) * 16 + (e & 15);
+#pragma unroll
+      for (int j = 0; j < DP; ++j) x[it][j] = 0.f;
+      if (qt >= QT) continue;
       if (col < n_cols) {
         const int row = col / a.group, hq = h * a.group + col % a.group;
         const T *p = (const T *)a.q + req * a.q_req + row * a.q_row + hq * a.q_head + pt * DP;
 #pragma unroll
-        for (int j = 0; j < DP; ++j) x[j] = ld_f32(p, j);
+        for (int j = 0; j < DP; ++j) x[it][j] = ld_f32(p, j);
       }
+      uint32_t top = 0;
 #pragma unroll
-      for (int j = 0; j < DP; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-      sm_top[pt][n] = top;
+      for (int j = 0; j < DP; ++j) top = max(top, __float_as_uint(x[it][j]) & 0x7fffffffu);
+      sm_top[qt][pt][e & 15] = top;
     }
     __syncthreads();
-    uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) top = max(top, sm_top[j][n]);
-    // exponent of the largest, held where both powers are normal numbers; not a number, infinite: as it is
-    const int ex = top >= 0x7f800000u ? 8 : max((int)(top >> 23) - 127, -100);
-    const float down = __uint_as_float((uint32_t)(127 + 8 - ex) << 23);
-    if (threadIdx.x < 16) sm_qf[n] = __uint_as_float((uint32_t)(127 - 8 + ex) << 23) * a.scale_log2;
-    for (int pt = part; pt < 16; pt += NW * 4) {
-      const int col = qg * 16 + n;
-      const int row = col / a.group, hq = h * a.group + col % a.group;
-      const T *p = (const T *)a.q + req * a.q_req + row * a.q_row + hq * a.q_head + pt * DP;
+    for (int it = 0; it < IT; ++it) {
+      const int e = threadIdx.x + it * NW * 64, qt = e >> 8, pt = e >> 4 & 15, m = e & 15;
+      if (qt >= QT) continue;
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) top = max(top, sm_top[qt][j][m]);
+      // halves: divided by a power of two that brings the largest below 512, held where both powers are normal numbers
+      const bool finite = top < 0x7f800000u;
+      const int ex = finite ? max((int)(top >> 23) - 127, -100) : 8;
+      const float down = __uint_as_float((uint32_t)(127 + 8 - ex) << 23);
+      // whole numbers up to 127 in their highest byte; the factor of a row that is not finite is NaN, and so are its scores
+      constexpr float MOST = NP == 2 ? 127.f * 256.f : 127.f * 65536.f;
+      const float big = fmaxf(__uint_as_float(top), 1e-31f), sign = a.scale_log2 < 0.f ? -1.f : 1.f;   // (factors are not negative)
+      const float up = finite ? MOST / big * sign : 0.f;
+      if (pt == 0) {
+        sm_qf[qt][0][m] = finite ? big / MOST * fabsf(a.scale_log2) : __uint_as_float(0x7fc00000u);
+        sm_qf[qt][1][m] = __uint_as_float((uint32_t)(127 - 8 + ex) << 23) * fabsf(a.scale_log2);
+      }
 #pragma unroll
       for (int j = 0; j < DP; ++j) {
         const int d = pt * DP + j;
-        const float x = col < n_cols ? ld_f32(p, j) * down : 0.f;
-        const f16_t hi = (f16_t)x;
-        // dim -> (step, group, element): 16 dims of a 16-byte load are 8 of two steps
-        int step, gg;
-        if (d < KW * 64) { step = (d >> 6) * 2 + ((d >> 3) & 1); gg = (d & 63) >> 4; }
-        else { step = 2 * KW; gg = (d & 31) >> 3; }
-        ((f16_t *)&sm_q[step][gg * 16 + n])[d & 7] = hi;
-        if (QP) ((f16_t *)&sm_q[(QP ? NS : 0) + step][gg * 16 + n])[d & 7] = (f16_t)(x - (float)hi);
+        // dim -> (step of 64, group, byte) for the codes; 16 dims of a 16-byte load are 8 of two steps of 32 for the halves
+        const bool wide = d < KW * 64;
+        const int gg = wide ? (d & 63) >> 4 : (d & 31) >> 3, step = wide ? (d >> 6) * 2 + ((d >> 3) & 1) : 2 * KW;
+        const float y = x[it][j] * down * sign;
+        const f16_t hi = (f16_t)y;
+        ((f16_t *)&sm_q[qt][step][gg * 16 + m])[d & 7] = hi;
+        if (QP) ((f16_t *)&sm_q[qt][(QP ? NS : 0) + step][gg * 16 + m])[d & 7] = (f16_t)(y - (float)hi);
+        int w = finite ? (int)rintf(x[it][j] * up) : 0;
+#pragma unroll
+        for (int b = NP - 1; b >= 0; --b) {
+          const int8_t c = (int8_t)w;
+          ((int8_t *)&sm_qi[qt][b][wide ? d >> 6 : KW][gg * 16 + m])[wide ? d & 15 : d & 7] = c;
+          w = (w - c) >> 8;
+        }
       }
     }
   }
   // ---- what the columns see ----
   const int cap = a.c.n_block * BYTE_BLOCK;
   const int n_keys = min(max(a.lens[req], 0), cap);
-  const int col = qg * 16 + n, row = min(col, n_cols - 1) / a.group;
-  int lim = col < n_cols ? n_keys : 0;
-  if (a.row_limit) lim = min(lim, max(a.row_limit[(size_t)req * a.n_row + row], 0));
-  const int tag = a.key_tag ? a.row_tag[(size_t)req * a.n_row + row] : 0;
-  const int reach = __builtin_amdgcn_readfirstlane(fold_row(lim, Max()));
-  const int lim_all = __builtin_amdgcn_readfirstlane(fold_row(col < n_cols ? lim : 0x7fffffff, Min()));
+  int lim[QT], tag[QT], reach = 0, lim_all = 0x7fffffff, tag_all = 0x7fffffff;
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const int col = (qg * QT + qt) * 16 + n, row = min(col, n_cols - 1) / a.group;
+    lim[qt] = col < n_cols ? n_keys : 0;
+    if (a.row_limit) lim[qt] = min(lim[qt], max(a.row_limit[(size_t)req * a.n_row + row], 0));
+    tag[qt] = a.key_tag ? a.row_tag[(size_t)req * a.n_row + row] : 0;
+    reach = max(reach, lim[qt]);
+    if (col < n_cols) { lim_all = min(lim_all, lim[qt]); tag_all = min(tag_all, tag[qt]); }
+  }
+  reach = __builtin_amdgcn_readfirstlane(fold_row(reach, Max()));
+  lim_all = __builtin_amdgcn_readfirstlane(fold_row(lim_all, Min()));
+  tag_all = __builtin_amdgcn_readfirstlane(fold_row(tag_all, Min()));
   const int whole = n_keys / BYTE_BLOCK;                 // blocks of codes; the next one is the tail
-  const int end = min((reach + BYTE_BLOCK - 1) / BYTE_BLOCK, a.nblk);
+  const int end = min((reach + BYTE_BLOCK - 1) / BYTE_BLOCK, a.nblk), sealed_end = min(end, whole);
   __syncthreads();
-  const float qf = sm_qf[n];
+  float qf[QT];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) qf[qt] = sm_qf[qt][0][n];
 
-  const int8_t *K = a.c.k + rhz * a.c.n_block * BYTE_BLOCK * HD, *V = a.c.v + rhz * a.c.n_block * BYTE_BLOCK * HD;
-  float m_run = -INFINITY, l_run = 0.f;
-  floatx4 o[NT];
+  float m_run[QT], l_run[QT], vref = 0.f;
+  floatx4 o[QT][NT];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int qt = 0; qt < QT; ++qt) {
+    m_run[qt] = -INFINITY; l_run[qt] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) o[qt][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  Frag ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones.hh[e] = (f16_t)1.f;
 
-  for (int kb = split * NW + wave; kb < end; kb += NW * a.nsplit) {
-    const bool sealed = kb < whole;
-    Frag vt[NT][2];
-    floatx4 s[4];
+  // KIND: 0 a block of codes with another one behind it, 1 the wave's last one, 2 the tail.  (Requests stand outside of all
+  // branches: where a branch decides on one, waits count on its not having been made, and where two make it, what arrives is
+  // waited for and copied.)
+  auto block = [&](auto kind_) {
+    constexpr int KIND = decltype(kind_)::value;
+    constexpr bool TAIL = KIND == 2;
+    const f16_t *kt = (const f16_t *)a.c.k_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD + key_m * HD;
+    const f16_t *vt = (const f16_t *)a.c.v_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD + n * BYTE_BLOCK + g * 16;
+    const int key0 = kb * BYTE_BLOCK + 16 * g;
+    if (TAIL) load_tags(kb);
+    union { uint4 u[2]; uint16_t s[16]; uint32_t w[8]; } tags;
+    tags.u[0] = tg[0]; tags.u[1] = tg[1];
+    const float ks = TAIL ? 1.f : ksc;
+    // ---- scores: lane (n, g), element e  <->  token kb * 64 + 16 g + e of column n ----
+    float sv[QT][16];
+    if (TAIL) {
+      floatx4 s[QT][4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-    float kf = qf, vf = 1.f;
-    const int key_m = 16 * (n >> 2) + (n & 3);           // key of operand row n of score tile 0 (tile t: + 4 t)
-    if (sealed) {
-      const int8_t *kp = K + (size_t)kb * BYTE_BLOCK * HD, *vp = V + (size_t)kb * BYTE_BLOCK * HD;
-      kf *= a.c.k_scale[rhz * a.c.n_block + kb];
-      vf = a.c.v_scale[rhz * a.c.n_block + kb];
+      for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int8_t *kr = kp + (key_m + 4 * t) * HD;
+        for (int t = 0; t < 4; ++t) s[qt][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < NS; ++c) {
-          uint2 x;
-          if (c < 2 * KW) x = *(const uint2 *)(kr + (c >> 1) * 64 + g * 16 + (c & 1) * 8);
-          else x = *(const uint2 *)(kr + KW * 64 + g * 8);
-          const Frag f = frag_of(x.x, x.y);
-          Frag q;
-          q.u = sm_q[c][lane];
-          s[t] = mfma16h(f, q, s[t]);
-          if (QP) { q.u = sm_q[(QP ? NS : 0) + c][lane]; s[t] = mfma16h(f, q, s[t]); }
+      for (int c = 0; c < NS; ++c)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          Frag f, q;
+          f.u = *(const uint4 *)(kt + 4 * t * HD + (c < 2 * KW ? (c >> 1) * 64 + g * 16 + (c & 1) * 8 : KW * 64 + g * 8));
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) {
+            q.u = sm_q[qt][c][lane];
+            s[qt][t] = mfma16h(f, q, s[qt][t]);
+            if (QP) { q.u = sm_q[qt][(QP ? NS : 0) + c][lane]; s[qt][t] = mfma16h(f, q, s[qt][t]); }
+          }
         }
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sv[qt][e] = s[qt][e >> 2][e & 3];
+    } else {
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        intx4 s[NP][4];
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int b = 0; b < NP; ++b) {
+            const uint4 q = sm_qi[qt][b][c][lane];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const intx4 from = c ? s[b][t] : intx4{0, 0, 0, 0};
+              // (the last 32 dims: half of the bytes are zeros, and the query's beside them anything.  The instruction for 32
+              // would do half the work, but its sums right behind those of the one for 64, whose results it adds to, came out wrong.)
+              s[b][t] = mfma_codes(c < KW ? kw[t][c < KW ? c : 0] : make_uint4(kn[t].x, kn[t].y, 0, 0), q, from);
+            }
+          }
+        // (the products of the two highest bytes stay below 2^30)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float high = (float)((s[0][e >> 2][e & 3] << 8) + s[1][e >> 2][e & 3]);
+          sv[qt][e] = NP == 2 ? high : fmaf(high, 256.f, (float)s[NP - 1][e >> 2][e & 3]);
+        }
+        if (QT > 1) __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    // whether every column sees the whole block (the same for the whole wave)
+    bool whole_seen = !TAIL && key0 - 16 * g + BYTE_BLOCK <= lim_all;
+    if (!TAIL && TG) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, max(tags.w[e] >> 16, tags.w[e] & 0xffff));
+      whole_seen = whole_seen && !__any((int)top > tag_all);
+      whole_seen = uniform(whole_seen);
+    }
+    if (KIND == 0) load_k(kb + stride);
+    __builtin_amdgcn_sched_barrier(0);
+    // ---- probabilities ----
+    const float vs = TAIL ? 1.f : __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(vsc)));
+    // vref, a power of two, is kept within 1 and 2^12 of the scales (the outputs then stay below 2^15 127 2^41 times the tokens)
+    float grow = 1.f;
+    if (!TAIL && uniform(vs > vref || (vs * 4096.f < vref && vs > 0.f))) {
+      const float to = __uint_as_float((__float_as_uint(vs) + 0x7fffffu) & 0xff800000u);
+      grow = vref / to;
+      vref = to;
+    }
+    if (TAIL && vref == 0.f) vref = 1.f;
+    // (a scale of zero: the sum of the probabilities grows, the outputs do not)
+    const float ratio = TAIL || vs == 0.f ? 1.f : vs * (1.f / vref), inv_ratio = __builtin_amdgcn_rcpf(ratio);
+    Frag ph[QT][2], pl[QT][2];
+    float take[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      float kf = TAIL ? sm_qf[qt][1][n] : qf[qt] * ks;
+      kf = kf == 0.f ? 1e-37f : kf;                      // (nothing but zeros comes of it, and -infinity stays what it is)
+      if (!whole_seen)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sv[qt][e] = ((key0 + e < lim[qt]) & ((int)tags.s[e] <= tag[qt])) ? sv[qt][e] : -INFINITY;
+      float mloc = sv[qt][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mloc = fmaxf(mloc, sv[qt][e]);
+      mloc = ceilf(fold32(fold16(mloc, Max()), Max()) * kf);
+      const float m_new = fmaxf(m_run[qt], mloc), m_ref = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run[qt] - m_ref), down = alpha * grow;
+      m_run[qt] = m_new;
+      // (fp32 outputs: the scale's logarithm in the exponent would round it by up to 2^-19; NaN has to arrive all the same)
+      const float off = P_BITS - m_ref + (sizeof(T) == 2 ? lg2(ratio) : 0.f * ratio);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sv[qt][e] = fmaf(sv[qt][e], kf, off);
+      if (!whole_seen && __any(kf != kf || off != off))  // NaN takes the tokens that are seen only
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          sv[qt][e] = ((key0 + e < lim[qt]) & ((int)tags.s[e] <= tag[qt])) ? sv[qt][e] : -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float p = __builtin_amdgcn_exp2f(sv[qt][e]);
+        if (sizeof(T) == 4) p *= fminf(ratio, 1.f);
+        ph[qt][e >> 3].hh[e & 7] = (f16_t)p;
+        if (PP) pl[qt][e >> 3].hh[e & 7] = (f16_t)(p - (float)ph[qt][e >> 3].hh[e & 7]);
+      }
+      floatx4 t = mfma16h(ones, ph[qt][0], floatx4{0.f, 0.f, 0.f, 0.f});
+      t = mfma16h(ones, ph[qt][1], t);
+      if (PP) { t = mfma16h(ones, pl[qt][0], t); t = mfma16h(ones, pl[qt][1], t); }
+      l_run[qt] = fmaf(t[0], inv_ratio == inv_ratio ? inv_ratio : 1.f, l_run[qt] * alpha);
+      take[qt] = t[0];
+      // (used here: sunk behind the branch below, the first use of the sums stood too close to the product for them to have
+      // arrived, where the branch is taken)
+      asm volatile("" : "+v"(l_run[qt]), "+v"(take[qt]));
+      if (!TAIL && uniform(vs == 0.f)) {
+        ph[qt][0].u = ph[qt][1].u = make_uint4(0, 0, 0, 0);
+        pl[qt][0].u = pl[qt][1].u = make_uint4(0, 0, 0, 0);
+      }
+      if (__any(down != 1.f))
+#pragma unroll
+        for (int i = 0; i < NT; ++i) o[qt][i] *= down;
+    }
+    // ---- outputs ----
+    __builtin_amdgcn_sched_barrier(0);
+    if (TAIL) {
+      const float f = 1.f / vref;
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        const uint4 x = *(const uint4 *)(vp + (i * 16 + n) * BYTE_BLOCK + g * 16);
-        vt[i][0] = frag_of(x.x, x.y);
-        vt[i][1] = frag_of(x.z, x.w);
-      }
-    } else {
-      const f16_t *kp = (const f16_t *)a.c.k_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD;
-      const f16_t *vp = (const f16_t *)a.c.v_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD;
+        // slots without a token hold anything: zeros instead, so that no product with a zero is NaN
+        Frag v0, v1;
+        v0.u = *(const uint4 *)(vt + i * 16 * BYTE_BLOCK);
+        v1.u = *(const uint4 *)(vt + i * 16 * BYTE_BLOCK + 8);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const f16_t *kr = kp + (key_m + 4 * t) * HD;
+        for (int e = 0; e < 8; ++e) {
+          if (key0 + e >= n_keys) v0.hh[e] = (f16_t)0.f;
+          if (key0 + 8 + e >= n_keys) v1.hh[e] = (f16_t)0.f;
+        }
 #pragma unroll
-        for (int c = 0; c < NS; ++c) {
-          Frag f, q;
-          f.u = *(const uint4 *)(kr + (c < 2 * KW ? (c >> 1) * 64 + g * 16 + (c & 1) * 8 : KW * 64 + g * 8));
-          q.u = sm_q[c][lane];
-          s[t] = mfma16h(f, q, s[t]);
-          if (QP) { q.u = sm_q[(QP ? NS : 0) + c][lane]; s[t] = mfma16h(f, q, s[t]); }
+        for (int qt = 0; qt < QT; ++qt) {
+          floatx4 t = mfma16h(v0, ph[qt][0], floatx4{0.f, 0.f, 0.f, 0.f});
+          t = mfma16h(v1, ph[qt][1], t);
+          if (PP) { t = mfma16h(v0, pl[qt][0], t); t = mfma16h(v1, pl[qt][1], t); }
+          // a column that sees nothing of the tail takes nothing from it, NaN or not
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[qt][i][e] = take[qt] != 0.f ? fmaf(t[e], f, o[qt][i][e]) : o[qt][i][e];
         }
       }
-      // slots without a token hold anything: zeros instead, so that no product with a zero is NaN
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          vt[i][st].u = *(const uint4 *)(vp + (i * 16 + n) * BYTE_BLOCK + g * 16 + st * 8);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (kb * BYTE_BLOCK + 16 * g + 8 * st + e >= n_keys) vt[i][st].hh[e] = (f16_t)0.f;
-        }
-    }
-    // lane (n, g), element e  <->  token kb * 64 + 16 g + e
-    float sv[16];
-    const int key0 = kb * BYTE_BLOCK + 16 * g;
-    if (!a.key_tag && kb * BYTE_BLOCK + BYTE_BLOCK <= lim_all) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sv[e] = s[e >> 2][e & 3] * kf;
     } else {
-      union { uint4 u[2]; uint16_t s[16]; } tg;
-      if (a.key_tag) {
-        const uint4 *tp = (const uint4 *)(a.key_tag + (size_t)req * cap + key0);
-        tg.u[0] = tp[0]; tg.u[1] = tp[1];
-      } else {
-        tg.u[0] = tg.u[1] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const Frag v0 = frag_of(vw[i].x, vw[i].y), v1 = frag_of(vw[i].z, vw[i].w);
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          o[qt][i] = mfma16h(v0, ph[qt][0], o[qt][i]);
+          o[qt][i] = mfma16h(v1, ph[qt][1], o[qt][i]);
+          if (PP) { o[qt][i] = mfma16h(v0, pl[qt][0], o[qt][i]); o[qt][i] = mfma16h(v1, pl[qt][1], o[qt][i]); }
+        }
       }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sv[e] = ((key0 + e < lim) & ((int)tg.s[e] <= tag)) ? s[e >> 2][e & 3] * kf : -INFINITY;
     }
-    float mloc = sv[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) mloc = fmaxf(mloc, sv[e]);
-    mloc = fold32(fold16(mloc, Max()), Max());
-    const float m_new = fmaxf(m_run, mloc), m_ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_ref);
-    Frag ph[2], pl[2];
-    float psum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float p = __builtin_amdgcn_exp2f(sv[e] - (m_ref - P_BITS));
-      psum += p;
-      ph[e >> 3].hh[e & 7] = (f16_t)p;
-      if (PP) pl[e >> 3].hh[e & 7] = (f16_t)(p - (float)ph[e >> 3].hh[e & 7]);
-    }
-    l_run = l_run * alpha + psum;
-    m_run = m_new;
-    if (__any(alpha != 1.f))
-#pragma unroll
-      for (int i = 0; i < NT; ++i) o[i] *= alpha;
-    // a column that sees nothing of the block takes nothing from it, whatever its scale is
-    const bool some = fold32(fold16(psum, Add()), Add()) != 0.f;
-    const float vfs = some ? vf : 0.f;
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      floatx4 t = mfma16h(vt[i][0], ph[0], floatx4{0.f, 0.f, 0.f, 0.f});
-      t = mfma16h(vt[i][1], ph[1], t);
-      if (PP) { t = mfma16h(vt[i][0], pl[0], t); t = mfma16h(vt[i][1], pl[1], t); }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[i][e] = sealed || some ? fmaf(t[e], vfs, o[i][e]) : o[i][e];
-    }
-  }
-  l_run = fold32(fold16(l_run, Add()), Add());
+    if (KIND == 0) load_v(kb + stride);
+    kb += stride;
+  };
+  while (kb + stride < sealed_end) block(std::integral_constant<int, 0>());
+  if (kb < sealed_end) block(std::integral_constant<int, 1>());
+  if (kb < end) block(std::integral_constant<int, 2>());          // (end is at most one beyond)
 
   // ---- the waves' states become one ----
-  if (g == 0) { sm_m[wave][n] = m_run; sm_l[wave][n] = l_run; }
 #pragma unroll
-  for (int i = 0; i < NT; ++i) sm_o[wave][i][lane] = o[i];
-  __syncthreads();
-  float fw[NW], M = -INFINITY, L = 0.f;
+  for (int qt = 0; qt < QT; ++qt)
+    if (g == 0) { sm_m[qt][wave][n] = m_run[qt]; sm_l[qt][wave][n] = l_run[qt]; }
 #pragma unroll
-  for (int w = 0; w < NW; ++w) { fw[w] = sm_m[w][n]; M = fmaxf(M, fw[w]); }
+  for (int qt = 0; qt < QT; ++qt) {
+    if (qt) __syncthreads();
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    // (a wave whose keys are all NaN has no maximum but a sum)
-    fw[w] = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fw[w] - M);
-    L += fw[w] * sm_l[w][n];
-  }
-  const size_t unit = rhz * a.nqg + qg;
-  if (a.nsplit > 1) {
-    float *pp = a.part + (unit * a.nsplit + split) * (size_t)(PSTR * 16);
-    if (wave == 0 && g == 0) { pp[n] = M; pp[16 + n] = L; }
+    for (int i = 0; i < NT; ++i) sm_o[wave][i][lane] = o[qt][i] * vref;
+    __syncthreads();
+    float fw[NW], M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) { fw[w] = sm_m[qt][w][n]; M = fmaxf(M, fw[w]); }
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      // (a wave whose keys are all NaN has no maximum but a sum)
+      fw[w] = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fw[w] - M);
+      L += fw[w] * sm_l[qt][w][n];
+    }
+    const int col = (qg * QT + qt) * 16 + n;
+    if (a.nsplit > 1) {
+      float *pp = a.part + (((size_t)unit * a.nqg + qg) * QT + qt) * a.nsplit * (size_t)(PSTR * 16) + split * (size_t)(PSTR * 16);
+      if (wave == 0 && g == 0) { pp[n] = M; pp[16 + n] = L; }
+      for (int i = wave; i < NT; i += NW) {
+        floatx4 y = fw[0] * sm_o[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) y += fw[w] * sm_o[w][i][lane];
+        *(floatx4 *)(pp + 32 + ((i * 4 + g) * 16 + n) * 4) = y;
+      }
+      continue;
+    }
+    if (col >= n_cols) continue;
+    const size_t at = ((size_t)req * a.n_row + col / a.group) * a.c.n_kv_head * a.group + h * a.group + col % a.group;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    if (a.lse && wave == 0 && g == 0) a.lse[at] = (M + (__builtin_amdgcn_logf(L) - P_BITS)) * 0.6931471805599453f;
     for (int i = wave; i < NT; i += NW) {
       floatx4 y = fw[0] * sm_o[0][i][lane];
 #pragma unroll
       for (int w = 1; w < NW; ++w) y += fw[w] * sm_o[w][i][lane];
-      *(floatx4 *)(pp + 32 + ((i * 4 + g) * 16 + n) * 4) = y;
+      y *= inv;
+      store4((T *)a.out + at * HD + i * 16 + 4 * g, y);
     }
-    return;
-  }
-  if (col >= n_cols) return;
-  const size_t at = ((size_t)req * a.n_row + row) * a.c.n_kv_head * a.group + h * a.group + col % a.group;
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  if (a.lse && wave == 0 && g == 0) a.lse[at] = (M + (__builtin_amdgcn_logf(L) - P_BITS)) * 0.6931471805599453f;
-  for (int i = wave; i < NT; i += NW) {
-    floatx4 y = fw[0] * sm_o[0][i][lane];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) y += fw[w] * sm_o[w][i][lane];
-    y *= inv;
-    store4((T *)a.out + at * HD + i * 16 + 4 * g, y);
   }
 }
 
@@ -468,7 +652,7 @@ __global__ __launch_bounds__(256) void k_byte_merge(ByteAttnArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int i = blockIdx.x % NT;
   const size_t unit = blockIdx.x / NT;
-  const int qg = unit % a.nqg, h = unit / a.nqg % a.c.n_kv_head, req = unit / a.nqg / a.c.n_kv_head;
+  const int n16 = a.nqg * a.qt, qg = unit % n16, h = unit / n16 % a.c.n_kv_head, req = unit / n16 / a.c.n_kv_head;
   const float *pb = a.part + unit * a.nsplit * (size_t)(PSTR * 16);
   float M = -INFINITY, L = 0.f;
   floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -606,7 +790,10 @@ extern "C" int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, in
   return PD_OK;
 }
 
-struct ByteShape { int nqg, nblk, nsplit; int64_t units; };
+// Tiles of 16 columns per work-group: more of them share the conversion of the codes.
+static int byte_tiles(int cols) { return cols > 16 ? 2 : 1; }
+
+struct ByteShape { int qt, nqg, nblk, nsplit; int64_t units, grid; };
 
 static int byte_shape(const pd_byte_cache *c, int n_head, int n_row, int max_len, ByteShape *out) {
   PD_REQUIRE(n_head >= 1 && n_head % c->n_kv_head == 0, PD_EINVAL, "n_head = %d is no multiple of %d key heads", n_head,
@@ -616,17 +803,21 @@ static int byte_shape(const pd_byte_cache *c, int n_head, int n_row, int max_len
              n_head);
   const int64_t cap = (int64_t)c->n_block * BYTE_BLOCK;
   const int64_t most = max_len ? std::min<int64_t>(max_len, cap) : cap;
-  out->nqg = (n_row * (n_head / c->n_kv_head) + 15) / 16;
+  const int cols = n_row * (n_head / c->n_kv_head);
+  out->qt = byte_tiles(cols);
+  out->nqg = (cols + 16 * out->qt - 1) / (16 * out->qt);
   out->nblk = (int)((most + BYTE_BLOCK - 1) / BYTE_BLOCK);
-  out->units = (int64_t)c->n_req * c->n_kv_head * out->nqg;
+  const int64_t heads = (int64_t)c->n_req * c->n_kv_head;
+  out->units = heads * out->nqg;
   out->nsplit = out->units ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / out->units, out->nblk / 8)) : 1;
-  return check_grid(out->units * std::max(out->nsplit, c->head_dim / 16));
+  out->grid = (out->nqg > 1 ? (heads + 7) / 8 * 8 * out->nqg : out->units) * out->nsplit;
+  return check_grid(std::max(out->grid, out->units * out->qt * (c->head_dim / 16)));
 }
 
 extern "C" size_t pd_byte_attention_workspace_bytes(const pd_byte_cache *cache, int n_head, int n_row, int max_len) {
   ByteShape sh;
   if (check_cache(cache) || byte_shape(cache, n_head, n_row, max_len, &sh)) return 0;
-  return sh.nsplit > 1 ? (size_t)sh.units * sh.nsplit * 16 * (cache->head_dim + 2) * sizeof(float) : 16;
+  return sh.nsplit > 1 ? (size_t)sh.units * sh.qt * sh.nsplit * 16 * (cache->head_dim + 2) * sizeof(float) : 16;
 }
 
 extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const int64_t *q_strides, int n_head,
@@ -652,17 +843,20 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
   a.c = view(cache); a.q = q; a.q_req = q_strides[0]; a.q_row = q_strides[1]; a.q_head = q_strides[2];
   a.lens = lens; a.row_limit = row_limit; a.key_tag = key_tag; a.row_tag = row_tag; a.out = out; a.lse = out_lse;
   a.part = (float *)workspace; a.n_row = n_row; a.group = n_head / cache->n_kv_head;
-  a.nqg = sh.nqg; a.nsplit = sh.nsplit; a.nblk = sh.nblk; a.scale_log2 = scale * 1.4426950408889634f; a.wide_q = 0;
+  a.nqg = sh.nqg; a.qt = sh.qt; a.nsplit = sh.nsplit; a.nblk = sh.nblk; a.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t s = (hipStream_t)hip_stream;
-  const unsigned grid = (unsigned)(sh.units * sh.nsplit);
-#define PD_ATTEND(T, HDV)                                                                                                \
-  do {                                                                                                                   \
-    hipLaunchKernelGGL((k_byte_attn<T, HDV, sizeof(T) == 4, !std::is_same<T, bf16_t>::value, 4>), dim3(grid), dim3(256), 0, s, a);                        \
-    if (sh.nsplit > 1)                                                                                                   \
-      hipLaunchKernelGGL((k_byte_merge<T, HDV>), dim3((unsigned)(sh.units * (HDV / 16))), dim3(256), 0, s, a);           \
+  const unsigned grid = (unsigned)sh.grid, tiles = (unsigned)(sh.units * sh.qt * (cache->head_dim / 16));
+#define PD_ATTEND_QT(T, HDV, QT) \
+  hipLaunchKernelGGL((k_byte_attn<T, HDV, !std::is_same<T, bf16_t>::value, QT, 4>), dim3(grid), dim3(256), 0, s, a)
+#define PD_ATTEND(T, HDV)                                                                                    \
+  do {                                                                                                       \
+    if (sh.qt == 2) PD_ATTEND_QT(T, HDV, 2);                                                                 \
+    else PD_ATTEND_QT(T, HDV, 1);                                                                            \
+    if (sh.nsplit > 1) hipLaunchKernelGGL((k_byte_merge<T, HDV>), dim3(tiles), dim3(256), 0, s, a);          \
   } while (0)
   PD_BYTE_TYPES(type, cache->head_dim, PD_ATTEND)
 #undef PD_ATTEND
+#undef PD_ATTEND_QT
   PD_CHECK_HIP(hipGetLastError());
   return PD_OK;
 }

@@ -41,11 +41,12 @@ def contents(tokens):
 
 def attend(q, k, v, sees, scale):
     """q [row][head][dim], k / v [token][kv head][dim], sees [row][token] -> (out, lse, per-element sum of p |v| / sum of p,
-    per (row, head) largest sum of |q||k|, largest |score|) in 64 bits."""
+    per (row, head) largest sum of |q||k|, largest |score|, largest sum of |k| times the query's largest) in 64 bits."""
     rows, heads, dim = q.shape
     group = heads // k.shape[1]
     out, mag = np.zeros((rows, heads, dim)), np.zeros((rows, heads, dim))
     lse, dot, top = np.full((rows, heads), -np.inf), np.zeros((rows, heads)), np.zeros((rows, heads))
+    flat = np.zeros((rows, heads))
     for r in range(rows):
         idx = np.flatnonzero(sees[r])
         if len(idx) == 0:
@@ -60,24 +61,31 @@ def attend(q, k, v, sees, scale):
             lse[r, h] = m + math.log(total)
             dot[r, h] = (np.abs(kk) @ np.abs(qq)).max() * abs(scale)
             top[r, h] = np.abs(s).max()
-    return out, lse, mag, dot, top
+            flat[r, h] = np.abs(kk).sum(axis=1).max() * np.abs(qq).max() * abs(scale)
+    return out, lse, mag, (dot, top, flat)
 
 
 HALF_STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
 SMALLEST = {"f32": 2.0 ** -150, "bf16": 2.0 ** -134, "f16": 2.0 ** -25}        # half of the type's smallest number
 
 
-def tolerance(kind, out, mag, dot, top, dim, tokens, largest):
+def tolerance(kind, out, mag, scores, dim, tokens, largest):
     """Largest error of (out, lse), from the roundings of the definition's steps.
 
-    A score: dim products (exact: 11 or 22 bits times 8) added in fp32, in up to two passes, each addition off by 2^-24 of
-    what the magnitudes sum up to; queries off by 2^-22 (pairs) or exact but for parts below 2^-24 of the row's largest; three
-    factors in fp32.  A probability: its score's error, the exponential (2^-22), and as an operand 2^-12 (bf16 queries) or
-    2^-22, but never nearer than half of the smallest half, 2^-25, where the row's largest is 2^15: 2^-40 of it, times the
-    values' largest magnitude for each token (the largest probability alone makes the sum that divides).  Sums over the tokens in fp32: 2^-24 each at most.  Then the output's own rounding, by half of
-    its smallest number at least."""
-    score = dot * ((2 * dim + 8) * 2.0 ** -24 + 2.0 ** -22) + dim * dot * 2.0 ** -24 + top * 2.0 ** -22
+    A score: queries are whole numbers of steps of the row's largest / 32512 (bf16) or / 127 2^16 (fp32, half), half a step off;
+    against the tail they are halves (11 bits hold a 16-bit query but for parts below 2^-24 of the row's largest) or pairs.
+    Products with codes are exact; those with the tail's halves are added in fp32 in up to two passes, each addition off by
+    2^-24 of what the magnitudes sum up to; three factors in fp32.  A probability: its score's error, the exponential (2^-22),
+    and as an operand 2^-12 (bf16 queries) or 2^-22, but never nearer than half of the smallest half, 2^-25, where the row's
+    largest is between 2^14 and 2^15: 2^-39 of it, times 2 where the value scale is that much below its power of two (2^12 at
+    most), times the values' largest magnitude for each token (the largest probability alone makes the sum that divides).  The
+    sums are of the probabilities as they enter the products.  Sums over the tokens in fp32: 2^-24 each at most.  Then the
+    output's own rounding, by half of its smallest number at least."""
+    dot, top, flat = scores
+    step = 1 / 65024 if kind == "bf16" else 2.0 ** -23.9
+    score = dot * ((2 * dim + 8) * 2.0 ** -24 + 2.0 ** -22) + flat * (step + 2.0 ** -24) + top * 2.0 ** -22
     prob = score + 2.0 ** -22 + (2.0 ** -12 if kind == "bf16" else 2.0 ** -22)
     rel = 2 * prob + 2 * (tokens + 64) * 2.0 ** -24
-    lse = score + 2.0 ** -22 + (tokens + 64) * 2.0 ** -24
-    return mag * rel[..., None] * 1.01 + np.maximum(np.abs(out) * HALF_STEP[kind], SMALLEST[kind]) + tokens * largest * 2.0 ** -40 + 1e-30, lse + (top + 16) * 2.0 ** -23
+    lse = prob + (tokens + 64) * 2.0 ** -24
+    rounded = np.maximum(np.abs(out) * HALF_STEP[kind], SMALLEST[kind])
+    return mag * rel[..., None] * 1.01 + rounded + tokens * largest * 2.0 ** -38 + 1e-30, lse + (top + 16) * 2.0 ** -23

@@ -209,8 +209,8 @@ def check_attention(kind, lens, rows, heads, kv, dim, row_limit=None, tags=None,
         if tags is not None:
             sees &= np.array(tags[0][r])[None, :n].astype(int) <= np.array(tags[1][r])[:, None]
         kk, vv = u.contents(kn[r, :n])[3], u.contents(vn[r, :n])[3]
-        want, wl, mag, dot, top = u.attend(qn[r].astype(np.float64), kk, vv, sees, 1 / math.sqrt(dim) if scale is None else scale)
-        tol, tl = u.tolerance(kind, want, mag, dot, top, dim, n, np.abs(vv).max(initial=0))
+        want, wl, mag, scores = u.attend(qn[r].astype(np.float64), kk, vv, sees, 1 / math.sqrt(dim) if scale is None else scale)
+        tol, tl = u.tolerance(kind, want, mag, scores, dim, n, np.abs(vv).max(initial=0))
         bad = np.abs(out[r] - want) - tol
         assert not (bad > 0).any() and np.isfinite(out[r]).all(), (r, bad.max(), np.abs(out[r] - want).max())
         none = ~sees.any(axis=1)
@@ -363,8 +363,8 @@ def test_store_attend_read_as_a_program_does_captured_and_replayed():
         for r in range(req):
             check_contents(cache, r, kn[r], vn[r], i + 1)
             kk, vv = u.contents(kn[r, :i + 1])[3], u.contents(vn[r, :i + 1])[3]
-            want, _, mag, dot, top = u.attend(qn[r, i:i + 1].astype(np.float64), kk, vv, np.ones((1, i + 1), bool), dim ** -0.5)
-            tol, _ = u.tolerance("bf16", want, mag, dot, top, dim, i + 1, np.abs(vv).max())
+            want, _, mag, scores = u.attend(qn[r, i:i + 1].astype(np.float64), kk, vv, np.ones((1, i + 1), bool), dim ** -0.5)
+            tol, _ = u.tolerance("bf16", want, mag, scores, dim, i + 1, np.abs(vv).max())
             assert (np.abs(out[r].float().cpu().numpy() - want) <= tol).all()
             assert np.array_equal(back[0][r, :2].cpu().numpy(), kk[i - 1:].astype(np.float32))
             assert (back[0][r, 2] == 0).all()
@@ -416,8 +416,8 @@ def test_offsets_beyond_32_bits():
     out = cache.attention(q, ints([n]), key_tag=tag, row_tag=ints([[0]]))
     sees = np.zeros((1, m), dtype=bool)
     sees[0, 5], sees[0, m - 100:] = True, True
-    want, _, mag, dot, top = u.attend(qn[0].astype(np.float64), held[0], held[1], sees, dim ** -0.5)
-    tol, _ = u.tolerance("f32", want, mag, dot, top, dim, 2048, np.abs(held[1]).max())
+    want, _, mag, scores = u.attend(qn[0].astype(np.float64), held[0], held[1], sees, dim ** -0.5)
+    tol, _ = u.tolerance("f32", want, mag, scores, dim, 2048, np.abs(held[1]).max())
     assert (np.abs(out[0].cpu().numpy() - want) <= tol).all()
 
 
