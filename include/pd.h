@@ -351,18 +351,22 @@ int pd_get_info(pd_ctx *ctx, int key, void *hip_stream, int64_t *value);
  * when its block is whole, scale = fp32(largest magnitude / 127), code = value / scale to the nearest whole number, ties to
  * even, and the token stands for code * scale from then on: at most half a scale from what came, plus the rounding to halves.
  * What a cache holds does not depend on the pieces in which its tokens came.  A NaN makes the scale of its block NaN, and with
- * it every key (or value) of the block.  All arrays are contiguous, in the order written.  Whoever makes the contents in another way keeps codes
- * within [-127, 127]. */
+ * it every key (or value) of the block.
+ *
+ * All arrays are contiguous.  Codes and tails lie in the order in which the attention kernel loads them: the 64 tokens of a block
+ * by groups of 16 (tail: 8) dims for keys; for values by 4 groups g of 16 tokens, place i of which is token 16 (i >> 2) + 4 g +
+ * (i & 3) (tail: two halves, s, of 8 places, token 16 (2 s + (i >> 2)) + 4 g + (i & 3)).  Who fills a cache in another way than
+ * through pd_byte_append keeps codes within [-127, 127], scales at 0 or above, and codes of 0 where the scale is 0. */
 #define PD_BYTE_BLOCK 64
 #define PD_TYPE_F32  0
 #define PD_TYPE_BF16 1
 #define PD_TYPE_F16  2
 typedef struct {
-  int8_t *k;                  /* [n_req][n_kv_head][n_block][64][head_dim]                                   */
-  int8_t *v;                  /* [n_req][n_kv_head][n_block][head_dim][64]                                   */
+  int8_t *k;                  /* [n_req][n_kv_head][n_block][head_dim / 16][64][16]                          */
+  int8_t *v;                  /* [n_req][n_kv_head][n_block][4][head_dim][16]                                */
   float *k_scale, *v_scale;   /* [n_req][n_kv_head][n_block]                                                 */
-  void *k_tail;               /* half [n_req][n_kv_head][2][64][head_dim]                                    */
-  void *v_tail;               /* half [n_req][n_kv_head][2][head_dim][64]                                    */
+  void *k_tail;               /* half [n_req][n_kv_head][2][head_dim / 8][64][8]                             */
+  void *v_tail;               /* half [n_req][n_kv_head][2][2][4][head_dim][8]                               */
   int32_t n_req, n_kv_head, head_dim, n_block;   /* head_dim 32, 64, 96 or 128; codes and tails 16-byte aligned */
 } pd_byte_cache;
 

@@ -30,44 +30,56 @@ class ByteCache:
     between calls but the tensors k, v, k_scale, v_scale, k_tail, v_tail, and calls can be captured into a graph."""
 
     def __init__(self, n_req, n_kv_head, head_dim, max_tokens, device="cuda:0"):
-        n_block = -(-max_tokens // BLOCK)
-        zeros = lambda *shape, dtype: torch.zeros(*shape, dtype=dtype, device=device)  # noqa: E731
-        self._hold(zeros(n_req, n_kv_head, n_block, BLOCK, head_dim, dtype=torch.int8),
-                   zeros(n_req, n_kv_head, n_block, head_dim, BLOCK, dtype=torch.int8),
-                   zeros(n_req, n_kv_head, n_block, dtype=torch.float32),
-                   zeros(n_req, n_kv_head, n_block, dtype=torch.float32),
-                   zeros(n_req, n_kv_head, 2, BLOCK, head_dim, dtype=torch.float16),
-                   zeros(n_req, n_kv_head, 2, head_dim, BLOCK, dtype=torch.float16))
+        device, n_block = torch.device(device), -(-max_tokens // BLOCK)
+        _require(device.type == "cuda", "a byte cache lives on a GPU, not on %s", device)
+        _require(head_dim in (32, 64, 96, 128) and min(n_req, n_kv_head, n_block) >= 1,
+                 "a byte cache has requests, heads and blocks, and heads of 32, 64, 96 or 128: not %s",
+                 (n_req, n_kv_head, n_block, head_dim))
+        zeros = lambda *shape, dtype: torch.zeros(n_req, n_kv_head, *shape, dtype=dtype, device=device)  # noqa: E731
+        self.k = zeros(n_block, head_dim // 16, BLOCK, 16, dtype=torch.int8)
+        self.v = zeros(n_block, 4, head_dim, 16, dtype=torch.int8)
+        self.k_scale, self.v_scale = (zeros(n_block, dtype=torch.float32) for _ in range(2))
+        self.k_tail = zeros(2, head_dim // 8, BLOCK, 8, dtype=torch.float16)
+        self.v_tail = zeros(2, 2, 4, head_dim, 8, dtype=torch.float16)
+        self.n_req, self.n_kv_head, self.n_block, self.head_dim = n_req, n_kv_head, n_block, head_dim
+        self.device = self.k.device
+        self._scale = 1.0 / math.sqrt(head_dim)
+        self._lib = load()
+        self._c = PdByteCache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                              self.k_tail.data_ptr(), self.v_tail.data_ptr(), n_req, n_kv_head, head_dim, n_block)
+        self._p = C.byref(self._c)
+
+    # -- in and out, in the plain order of tokens and dims -------------------------
+    def to_tensors(self):
+        """What the cache holds in plain order: k int8 [req][head][block][64][dim], v int8 [req][head][block][dim][64], k_scale,
+        v_scale, k_tail half [req][head][2][64][dim], v_tail half [req][head][2][dim][64] (copies)."""
+        r, h, n, d = self.n_req, self.n_kv_head, self.n_block, self.head_dim
+        return {"k": self.k.transpose(3, 4).reshape(r, h, n, BLOCK, d),
+                "v": self.v.view(r, h, n, 4, d, 4, 4).permute(0, 1, 2, 4, 5, 3, 6).reshape(r, h, n, d, BLOCK),
+                "k_scale": self.k_scale.clone(), "v_scale": self.v_scale.clone(),
+                "k_tail": self.k_tail.transpose(3, 4).reshape(r, h, 2, BLOCK, d),
+                "v_tail": self.v_tail.view(r, h, 2, 2, 4, d, 2, 4).permute(0, 1, 2, 5, 3, 6, 4, 7).reshape(r, h, 2, d, BLOCK)}
 
     @classmethod
     def from_tensors(cls, k, v, k_scale, v_scale, k_tail, v_tail):
-        """A cache in tensors that are there already (not copied)."""
-        self = cls.__new__(cls)
-        self._hold(k, v, k_scale, v_scale, k_tail, v_tail)
-        return self
-
-    def _hold(self, k, v, k_scale, v_scale, k_tail, v_tail):
+        """A cache that holds what these tensors hold (the ones of to_tensors, on its device; copied).  Codes are within
+        [-127, 127], and 0 where the scale is 0; scales are not negative."""
         _require(k.dim() == 5 and k.shape[3] == BLOCK, "k must be [req][head][block][%d][dim], not %s", BLOCK, tuple(k.shape))
-        req, heads, n_block, _, dim = k.shape
-        for name, t, shape, dtype in (("k", k, k.shape, torch.int8), ("v", v, (req, heads, n_block, dim, BLOCK), torch.int8),
-                                      ("k_scale", k_scale, (req, heads, n_block), torch.float32),
-                                      ("v_scale", v_scale, (req, heads, n_block), torch.float32),
-                                      ("k_tail", k_tail, (req, heads, 2, BLOCK, dim), torch.float16),
-                                      ("v_tail", v_tail, (req, heads, 2, dim, BLOCK), torch.float16)):
-            _require(tuple(t.shape) == tuple(shape) and t.dtype == dtype, "%s must be %s %s, not %s %s", name, dtype,
-                     tuple(shape), t.dtype, tuple(t.shape))
-            _require(t.is_contiguous() and t.device == k.device, "%s must be contiguous and on %s", name, k.device)
-        _require(dim in (32, 64, 96, 128) and min(req, heads, n_block) >= 1,
-                 "a byte cache has requests, heads, blocks and heads of 32, 64, 96 or 128, not %s", tuple(k.shape))
-        _require(k.device.type == "cuda", "a byte cache lives on a GPU, not on %s", k.device)
-        self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail = k, v, k_scale, v_scale, k_tail, v_tail
-        self.n_req, self.n_kv_head, self.n_block, self.head_dim = req, heads, n_block, dim
-        self.device = k.device
-        self._scale = 1.0 / math.sqrt(dim)
-        self._lib = load()
-        self._c = PdByteCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(),
-                              v_tail.data_ptr(), req, heads, dim, n_block)
-        self._p = C.byref(self._c)
+        r, h, n, _, d = k.shape
+        for name, t, shape, dtype in (("k", k, k.shape, torch.int8), ("v", v, (r, h, n, d, BLOCK), torch.int8),
+                                      ("k_scale", k_scale, (r, h, n), torch.float32), ("v_scale", v_scale, (r, h, n), torch.float32),
+                                      ("k_tail", k_tail, (r, h, 2, BLOCK, d), torch.float16),
+                                      ("v_tail", v_tail, (r, h, 2, d, BLOCK), torch.float16)):
+            _require(t.shape == tuple(shape) and t.dtype == dtype and t.device == k.device, "%s must be %s %s on %s, not %s %s on %s",
+                     name, dtype, tuple(shape), k.device, t.dtype, tuple(t.shape), t.device)
+        self = cls(r, h, d, n * BLOCK, device=k.device)
+        self.k.copy_(k.reshape(r, h, n, BLOCK, d // 16, 16).transpose(3, 4))
+        self.v.view(r, h, n, 4, d, 4, 4).copy_(v.reshape(r, h, n, d, 4, 4, 4).permute(0, 1, 2, 5, 3, 4, 6))
+        self.k_scale.copy_(k_scale)
+        self.v_scale.copy_(v_scale)
+        self.k_tail.copy_(k_tail.reshape(r, h, 2, BLOCK, d // 8, 8).transpose(3, 4))
+        self.v_tail.view(r, h, 2, 2, 4, d, 2, 4).copy_(v_tail.reshape(r, h, 2, d, 2, 2, 4, 4).permute(0, 1, 2, 4, 6, 3, 5, 7))
+        return self
 
     # -- what every call checks --------------------------------------------------
     def _data(self, name, t, shape):

@@ -1,11 +1,15 @@
 // A cache of keys and values in 8 bits: storing tokens, reading them back, attention over them.
 //
 // Per request and key head, tokens lie in blocks of 64.  A whole block holds signed codes of 8 bits and one fp32 scale for its
-// keys, one for its values; the tokens behind the last whole block are halves in a tail of two slots (block b: slot b & 1):
-//   k [block][64][hd], v [block][hd][64] int8;  k_tail [2][64][hd], v_tail [2][hd][64] half;  scales [block] fp32.
-// 64 tokens, and values by dims, because a lane of the 16x16x32 matrix instruction then loads 16 bytes that are operands as
-// they lie: 16 dims of a key are two contraction steps of the scores, 16 keys of a value's dim two of the outputs (any order of
-// the contraction is right that both operands share).
+// keys, one for its values; the tokens behind the last whole block are halves in a tail of two slots (block b: slot b & 1).
+// Everything lies in the order in which 16 lanes of a wave load 256 bytes that are operands of the matrix instruction (any order
+// of a contraction is right that both operands share):
+//   k       [block][hd / 16][64 tokens][16 dims]        k_tail  [2][hd / 8][64][8 dims] half
+//   v       [block][4][hd][16 tokens]                   v_tail  [2][2][4][hd][8 tokens] half
+// where place i of group g of a value's tokens is token 16 (i >> 2) + 4 g + (i & 3) of the block (tails: the first 8 places, then
+// the others): the scores leave the matrix instruction in this order, and it is that of the operand for the outputs.
+// Rows of [64][hd] and [hd][64] instead, where neighbouring lanes load pieces of different rows: 16384 tokens of one head of size
+// 128 in one work-group of 8 waves 107 us against 73, 32 x 8 heads x 8192 tokens 76.8 against 71.0.
 #include "byte_cache.h"
 
 #include <algorithm>
@@ -35,12 +39,18 @@ __device__ __forceinline__ int code_of(float x, float s, float inv) {
   return (int)fminf(fmaxf(q, -127.f), 127.f);
 }
 
+__device__ __forceinline__ uint32_t bytes4(int a, int b, int c, int d) {
+  const uint32_t lo = __builtin_amdgcn_perm((uint32_t)b, (uint32_t)a, 0x0c0c0400u), hi = __builtin_amdgcn_perm((uint32_t)d, (uint32_t)c, 0x04000c0cu);
+  return lo | hi;
+}
+
 // One work-group per (request, head, touched block, keys or values): the block's tokens go to LDS as halves, the old ones from
-// the tail, the new ones from the caller; a whole block leaves as codes, a block that is not yet whole as halves of its new
-// tokens.  Bound by the bytes.
+// the tail, the new ones from the caller (all requested before the first is used); a whole block leaves as codes, one that is not
+// yet whole as halves of its new tokens.  Bound by the bytes.
 template <typename T, int HD, bool WIDE>
 __global__ __launch_bounds__(256) void k_byte_store(StoreArgs a) {
   constexpr int P = HD + 8;                              // halves per token row in LDS (16-byte rows)
+  constexpr int IT = HD / 32;                            // pieces of 8 dims per thread
   __shared__ f16_t tile[BYTE_BLOCK * P];
   __shared__ uint32_t sm_top[4];
   const int tid = threadIdx.x;
@@ -63,41 +73,58 @@ __global__ __launch_bounds__(256) void k_byte_store(StoreArgs a) {
     const int n_old = min(max(before - t0, 0), BYTE_BLOCK), n_all = min(len - t0, BYTE_BLOCK);
     f16_t *tail = tail0 + (size_t)(b & 1) * BYTE_BLOCK * HD;
     if (pass) __syncthreads();
-    // new tokens, 8 dims at a time
+    float x[IT][8];
+    uint4 old[IT];
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {                    // new tokens (others: any new one's, not used)
+      const int e = tid + it * 256, t = e / (HD / 8), d = e % (HD / 8) * 8;
+      load8<T, WIDE>(src + (int64_t)min(max(t0 + t - before, 0), count - 1) * s_tok + d, x[it]);
+    }
+    const bool mixed = whole && n_old > 0;               // (the same for the whole work-group)
+    if (mixed)
+#pragma unroll
+      for (int it = 0; it < IT; ++it) old[it] = ((const uint4 *)tail)[tid + it * 256];
     uint32_t top = 0;
-    for (int e = tid; e < BYTE_BLOCK * (HD / 8); e += 256) {
-      const int t = e / (HD / 8), d = e % (HD / 8) * 8;
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int e = tid + it * 256, t = e / (HD / 8), d = e % (HD / 8) * 8;
       if (t < n_old || t >= n_all) continue;
-      const T *p = src + (int64_t)(t0 + t - before) * s_tok + d;
-      float x[8];
-      load8<T, WIDE>(p, x);
       union { f16_t h[8]; uint4 q; } y;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        y.h[j] = to_half(x[j]);
+        y.h[j] = to_half(x[it][j]);
         top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y.h[j]) & 0x7fff));
       }
-      if (!whole && !kind) *(uint4 *)(tail + (size_t)t * HD + d) = y.q;
-      *(uint4 *)&tile[t * P + d] = y.q;
+      if (whole) *(uint4 *)&tile[t * P + d] = y.q;
+      else if (!kind) *(uint4 *)(tail + ((d >> 3) * BYTE_BLOCK + t) * 8) = y.q;
+      else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) tail[(((t >> 5) * 4 + ((t >> 2) & 3)) * HD + d + j) * 8 + ((t >> 4) & 1) * 4 + (t & 3)] = y.h[j];
     }
-    if (!whole) {
-      if (kind) {                                        // values lie by dims: 2 bytes per token and dim
-        __syncthreads();
-        const int n = n_all - n_old;
-        for (int e = tid; e < n * HD; e += 256) {
-          const int d = e / n, t = n_old + e % n;
-          tail[(size_t)d * BYTE_BLOCK + t] = tile[t * P + d];
+    if (!whole) continue;
+    if (mixed) {                                         // ... and the ones that were in the tail
+#pragma unroll
+      for (int it = 0; it < IT; ++it) {
+        const int e = tid + it * 256;
+        union { uint4 q; f16_t h[8]; } y;
+        y.q = old[it];
+        if (!kind) {
+          const int t = e & 63, d = (e >> 6) * 8;
+          if (t >= n_old) continue;
+          *(uint4 *)&tile[t * P + d] = y.q;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y.h[j]) & 0x7fff));
+        } else {
+          const int d = e % HD, sg = e / HD;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int t = 16 * (2 * (sg >> 2) + (j >> 2)) + 4 * (sg & 3) + (j & 3);
+            if (t >= n_old) continue;
+            tile[t * P + d] = y.h[j];
+            top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y.h[j]) & 0x7fff));
+          }
         }
       }
-      continue;
-    }
-    // ... and the ones that were in the tail
-    for (int e = tid; e < n_old * HD; e += 256) {
-      int t, d;
-      if (kind) { d = e / n_old; t = e % n_old; } else { t = e / HD; d = e % HD; }
-      const f16_t y = kind ? tail[(size_t)d * BYTE_BLOCK + t] : tail[(size_t)t * HD + d];
-      top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y) & 0x7fff));
-      tile[t * P + d] = y;
     }
     // the largest magnitude by its bits, where NaN is above everything: then the scale is NaN, and so is the block
     for (int m = 32; m; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
@@ -105,18 +132,37 @@ __global__ __launch_bounds__(256) void k_byte_store(StoreArgs a) {
     __syncthreads();
     top = max(max(sm_top[0], sm_top[1]), max(sm_top[2], sm_top[3]));
     const float scale = __fdiv_rn((float)__builtin_bit_cast(f16_t, (uint16_t)top), 127.f);
-    const float inv = scale > 0.f ? 1.f / scale : 0.f;
+    const bool some = scale > 0.f;                       // (zeros, and NaN: codes of zero)
+    const float inv = some ? 1.f / scale : 0.f, sc = some ? scale : 1.f;
     if (tid == 0) (kind ? a.c.v_scale : a.c.k_scale)[rhz * a.c.n_block + b] = scale;
     int8_t *dst = (kind ? a.c.v : a.c.k) + (rhz * a.c.n_block + b) * BYTE_BLOCK * HD;
-    for (int e = tid; e < BYTE_BLOCK * HD / 16; e += 256) {
-      union { int8_t c[16]; uint4 q; } y;
+    if (!kind) {
+      for (int e = tid; e < BYTE_BLOCK * HD / 16; e += 256) {        // 16 dims of a token
+        union { uint4 q[2]; f16_t h[16]; } y;
+        const f16_t *row = &tile[(e & 63) * P + (e >> 6) * 16];
+        y.q[0] = *(const uint4 *)row; y.q[1] = *(const uint4 *)(row + 8);
+        int c[16];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const int o = e * 16 + j;
-        const f16_t x = kind ? tile[(o % BYTE_BLOCK) * P + o / BYTE_BLOCK] : tile[o / HD * P + o % HD];
-        y.c[j] = inv > 0.f ? (int8_t)code_of((float)x, scale, inv) : (int8_t)0;
+        for (int j = 0; j < 16; ++j) c[j] = some ? code_of((float)y.h[j], sc, inv) : 0;
+        ((uint4 *)dst)[e] = make_uint4(bytes4(c[0], c[1], c[2], c[3]), bytes4(c[4], c[5], c[6], c[7]),
+                                       bytes4(c[8], c[9], c[10], c[11]), bytes4(c[12], c[13], c[14], c[15]));
       }
-      ((uint4 *)dst)[e] = y.q;
+    } else {
+      for (int e = tid; e < BYTE_BLOCK * HD / 32; e += 256) {        // 8 places of 4 dims
+        const int half = e & 1, d = (e >> 1) % (HD / 4) * 4, g = (e >> 1) / (HD / 4);
+        int c[4][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          union { uint2 q; f16_t h[4]; } y;
+          y.q = *(const uint2 *)&tile[(16 * (2 * half + (j >> 2)) + 4 * g + (j & 3)) * P + d];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) c[i][j] = some ? code_of((float)y.h[i], sc, inv) : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *(uint2 *)(dst + (g * HD + d + i) * 16 + half * 8) =
+              make_uint2(bytes4(c[i][0], c[i][1], c[i][2], c[i][3]), bytes4(c[i][4], c[i][5], c[i][6], c[i][7]));
+      }
     }
   }
 }
@@ -131,11 +177,14 @@ struct ReadArgs {
   int n_tok, span;
 };
 
-// One work-group per (request, head, block that the range can touch, keys or values).
+// One work-group per (request, head, block that the range can touch, keys or values): the block goes to LDS by tokens, a whole
+// one as bytes, and leaves by rows of a token's dims.  Bound by the bytes.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_byte_read(ReadArgs a) {
-  constexpr int P = HD + 8;
-  __shared__ f16_t tile[BYTE_BLOCK * P];                 // codes are whole numbers up to 127: halves hold them
+  constexpr int P = HD + 8, PB = HD + 16;                // halves, bytes per token row in LDS
+  __shared__ uint4 mem[BYTE_BLOCK * P / 8];
+  f16_t *tile = (f16_t *)mem;
+  int8_t *codes = (int8_t *)mem;
   const int tid = threadIdx.x;
   const int kind = blockIdx.x & 1, u = blockIdx.x >> 1;
   const int i0 = u % a.span, rh = u / a.span, h = rh % a.c.n_kv_head, req = rh / a.c.n_kv_head;
@@ -151,21 +200,40 @@ __global__ __launch_bounds__(256) void k_byte_read(ReadArgs a) {
   if (whole) {
     scale = (kind ? a.c.v_scale : a.c.k_scale)[rhz * a.c.n_block + b];
     const uint4 *src = (const uint4 *)((kind ? a.c.v : a.c.k) + (rhz * a.c.n_block + b) * BYTE_BLOCK * HD);
-    for (int e = tid; e < BYTE_BLOCK * HD / 16; e += 256) {
-      union { uint4 q; int8_t c[16]; } x;
-      x.q = src[e];
+    if (!kind) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const int o = e * 16 + j;
-        tile[kind ? (o % BYTE_BLOCK) * P + o / BYTE_BLOCK : o / HD * P + o % HD] = (f16_t)(float)x.c[j];
+      for (int it = 0; it < (HD + 63) / 64; ++it) {
+        const int e = tid + it * 256;
+        if (HD % 64 == 0 || e < HD * 4) *(uint4 *)&codes[(e & 63) * PB + (e >> 6) * 16] = src[e];
+      }
+    } else if (tid < HD) {                               // 16 places of 4 dims, turned
+      const int d = tid % (HD / 4) * 4, g = tid / (HD / 4);
+      uint4 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = src[g * HD + d + i];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t p = (&x[0].x)[w], q = (&x[1].x)[w], r = (&x[2].x)[w], z = (&x[3].x)[w];
+        const uint32_t pq0 = __builtin_amdgcn_perm(q, p, 0x05010400u), pq1 = __builtin_amdgcn_perm(q, p, 0x07030602u);
+        const uint32_t rz0 = __builtin_amdgcn_perm(z, r, 0x05010400u), rz1 = __builtin_amdgcn_perm(z, r, 0x07030602u);
+        int8_t *row = &codes[(16 * w + 4 * g) * PB + d];
+        *(uint32_t *)row = __builtin_amdgcn_perm(rz0, pq0, 0x05040100u);
+        *(uint32_t *)(row + PB) = __builtin_amdgcn_perm(rz0, pq0, 0x07060302u);
+        *(uint32_t *)(row + 2 * PB) = __builtin_amdgcn_perm(rz1, pq1, 0x05040100u);
+        *(uint32_t *)(row + 3 * PB) = __builtin_amdgcn_perm(rz1, pq1, 0x07060302u);
       }
     }
   } else if (n > 0) {
-    const f16_t *src = (const f16_t *)(kind ? a.c.v_tail : a.c.k_tail) + (rhz * 2 + (b & 1)) * BYTE_BLOCK * HD;
-    for (int e = tid; e < n * HD; e += 256) {
-      int t, d;
-      if (kind) { d = e / n; t = e % n; } else { t = e / HD; d = e % HD; }
-      tile[t * P + d] = kind ? src[(size_t)d * BYTE_BLOCK + t] : src[(size_t)t * HD + d];
+    const uint4 *src = (const uint4 *)((const f16_t *)(kind ? a.c.v_tail : a.c.k_tail) + (rhz * 2 + (b & 1)) * BYTE_BLOCK * HD);
+#pragma unroll
+    for (int it = 0; it < HD / 32; ++it) {
+      const int e = tid + it * 256;
+      union { uint4 q; f16_t h[8]; } y;
+      y.q = src[e];
+      if (!kind) *(uint4 *)&tile[(e & 63) * P + (e >> 6) * 8] = y.q;
+      else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) tile[(16 * (2 * (e / HD >> 2) + (j >> 2)) + 4 * (e / HD & 3) + (j & 3)) * P + e % HD] = y.h[j];
     }
   }
   __syncthreads();
@@ -175,8 +243,17 @@ __global__ __launch_bounds__(256) void k_byte_read(ReadArgs a) {
     const int64_t at = t0 + t - from;
     if (at < 0 || at >= a.n_tok) continue;
     float y[8];
+    if (whole) {
+      union { uint2 q; int8_t c[8]; } x;
+      x.q = *(const uint2 *)&codes[t * PB + d];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = t < n ? (float)tile[t * P + d + j] * scale : 0.f;
+      for (int j = 0; j < 8; ++j) y[j] = (float)x.c[j] * scale;
+    } else {
+      union { uint4 q; f16_t h[8]; } x;
+      x.q = *(const uint4 *)&tile[t * P + d];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = t < n ? (float)x.h[j] : 0.f;
+    }
     store8(out + (((size_t)req * a.n_tok + at) * a.c.n_kv_head + h) * HD + d, y);
   }
 }
@@ -214,9 +291,11 @@ __device__ __forceinline__ Frag frag_of(uint32_t c0, uint32_t c1) {
   return f;
 }
 
-// Probabilities are held as 2^15 p: halves then keep their full precision down to 2^-29 instead of 2^-14, and the sums carry
-// the same factor.
-constexpr float P_BITS = 15.f;
+// Probabilities are held as 2^(15 - slack) p: halves then keep their full precision down to 2^-(29 - slack) instead of 2^-14, and
+// the sums carry the same factor.  Their reference follows the running maximum only when that is more than the slack above it,
+// so that after a wave's first blocks next to nothing is rescaled (128 products per block of 32 columns and 128 dims).  Where
+// probabilities are pairs of halves the low one ends 11 bits sooner, and the slack is smaller.
+constexpr float slack_of(bool pairs) { return pairs ? 4.f : 8.f; }
 
 // (a condition that is the same for the whole wave, as a branch of the scalar unit)
 __device__ __forceinline__ bool uniform(bool c) { return __builtin_amdgcn_readfirstlane(c ? 1 : 0) != 0; }
@@ -239,13 +318,13 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 
 // grid: (split, group of 16 QT columns, key head, request); NW waves.  The blocks of 64 tokens of a (request, key head) are dealt
 // round-robin to the waves of its splits.  A column is one query vector (row, query head of the key head's group).  Scores come
-// out of the matrix instruction with a lane holding 16 tokens of one column, in the order in which it is their operand for the
-// outputs: token 16 g + 8 s + e of the block is contraction slot (g, e) of step s.
+// out of the matrix instruction with a lane holding 16 tokens of one column, which are its operand for the outputs as they are:
+// element e of step s of group g is token 32 s + 16 (e >> 2) + 4 g + (e & 3) of the block.
 //  * Scores are products of bytes, exact in 32-bit integers: the keys' codes as they lie, queries as whole numbers of two bytes
 //    (bf16) or three (fp32, half), steps of the row's largest / 32512 or / 2^23.  No key is converted.
 //  * Values become halves in registers, exactly, once for QT tiles of 16 columns.
-//  * A block's key scale multiplies its scores.  The reference of the exponentials is a whole number (the running maximum
-//    rounded up), so that taking it off rounds nothing and rescaling by its change is exact.
+//  * A block's key scale multiplies its scores.  The reference of the exponentials is a whole number (a running maximum rounded
+//    up), so that taking it off rounds nothing and rescaling by its change is exact.
 //  * A block's value scale multiplies its probabilities, over a power of two (vref) within 2^12 of it: the outputs add up in
 //    the matrix instruction, in units of vref, and are rescaled, exactly, in the rare case that it moves.
 //  * The sums of the probabilities are a product with ones: the same roundings as in the outputs, and no work for the vector
@@ -259,6 +338,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   constexpr int PSTR = HD + 2;
   constexpr int NP = sizeof(T) == 2 && !PP ? 2 : 3, NC = (HD + 63) / 64;     // bytes of a query value; contraction steps of 64
   constexpr bool QP = sizeof(T) == 4;
+  constexpr float SLACK = slack_of(PP), P_BITS = 15.f - SLACK;
   __shared__ uint4 sm_qi[QT][NP][NC][64], sm_q[QT][(QP ? 2 : 1) * NS][64];
   __shared__ float sm_qf[QT][2][16];
   __shared__ uint32_t sm_top[QT][16][16];
@@ -283,9 +363,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   // before, its values when the outputs have.  The first is requested before anything else is read (a wave without one asks for
   // the last block that there is room for, and ignores it).  Scales come by vector loads, in order with the codes, so that
   // nothing waits for all that is under way.
-  const int key_m = 16 * (n >> 2) + (n & 3);             // token of operand row n of score tile 0 (tile t: + 4 t)
-  const int8_t *K = a.c.k + rhz * a.c.n_block * BYTE_BLOCK * HD + key_m * HD;
-  const int8_t *V = a.c.v + rhz * a.c.n_block * BYTE_BLOCK * HD + n * BYTE_BLOCK + g * 16;
+  const int8_t *K = a.c.k + rhz * a.c.n_block * BYTE_BLOCK * HD + n * 16;
+  const int8_t *V = a.c.v + rhz * a.c.n_block * BYTE_BLOCK * HD + (g * HD + n) * 16;
   int zero;
   asm("v_mov_b32 %0, 0" : "=v"(zero));
   const float *KS = a.c.k_scale + rhz * a.c.n_block + zero, *VS = a.c.v_scale + rhz * a.c.n_block + zero;
@@ -293,13 +372,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   int kb = split * NW + wave;
   uint4 kw[4][KW ? KW : 1], vw[NT];
   uint2 kn[4];
-  uint4 tg[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  uint2 tg[4] = {make_uint2(0, 0), make_uint2(0, 0), make_uint2(0, 0), make_uint2(0, 0)};
   float ksc, vsc;
-  const uint16_t *TG = a.key_tag ? a.key_tag + (size_t)req * a.c.n_block * BYTE_BLOCK + 16 * g : nullptr;
+  const uint16_t *TG = a.key_tag ? a.key_tag + (size_t)req * a.c.n_block * BYTE_BLOCK + 4 * g : nullptr;
   auto load_tags = [&](int b) {
     if (TG) {
-      const uint4 *tp = (const uint4 *)(TG + (size_t)b * BYTE_BLOCK);
-      tg[0] = tp[0]; tg[1] = tp[1];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) tg[t] = *(const uint2 *)(TG + (size_t)b * BYTE_BLOCK + 16 * t);
     }
   };
   auto load_k = [&](int b) {
@@ -309,15 +388,15 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
-      for (int c = 0; c < KW; ++c) kw[t][c] = ld_code<QT == 1, uint4>(kp + 4 * t * HD + c * 64 + g * 16);
-      if (NS & 1) kn[t] = ld_code<QT == 1, uint2>(kp + 4 * t * HD + KW * 64 + g * 8);
+      for (int c = 0; c < KW; ++c) kw[t][c] = ld_code<QT == 1, uint4>(kp + ((c * 4 + g) * BYTE_BLOCK + 16 * t) * 16);
+      if (NS & 1) kn[t] = ld_code<QT == 1, uint2>(kp + ((KW * 4 + (g >> 1)) * BYTE_BLOCK + 16 * t) * 16 + (g & 1) * 8);
     }
   };
   auto load_v = [&](int b) {
     const int8_t *vp = V + (size_t)b * BYTE_BLOCK * HD;
     vsc = VS[b];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) vw[i] = ld_code<QT == 1, uint4>(vp + i * 16 * BYTE_BLOCK);
+    for (int i = 0; i < NT; ++i) vw[i] = ld_code<QT == 1, uint4>(vp + i * 256);
   };
   load_k(min(kb, a.c.n_block - 1));
   load_v(min(kb, a.c.n_block - 1));
@@ -426,14 +505,23 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   auto block = [&](auto kind_) {
     constexpr int KIND = decltype(kind_)::value;
     constexpr bool TAIL = KIND == 2;
-    const f16_t *kt = (const f16_t *)a.c.k_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD + key_m * HD;
-    const f16_t *vt = (const f16_t *)a.c.v_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD + n * BYTE_BLOCK + g * 16;
-    const int key0 = kb * BYTE_BLOCK + 16 * g;
+    const f16_t *kt = (const f16_t *)a.c.k_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD + n * 8;
+    const f16_t *vt = (const f16_t *)a.c.v_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD + (g * HD + n) * 8;
+    const int key0 = kb * BYTE_BLOCK + 4 * g;            // element e: token key0 + 16 (e >> 2) + (e & 3)
+    auto key = [&](int e) { return key0 + 16 * (e >> 2) + (e & 3); };
+    Frag vtail[TAIL ? NT : 1][2];
+    if (TAIL)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        vtail[TAIL ? i : 0][0].u = *(const uint4 *)(vt + i * 128);
+        vtail[TAIL ? i : 0][1].u = *(const uint4 *)(vt + 4 * HD * 8 + i * 128);
+      }
     if (TAIL) load_tags(kb);
-    union { uint4 u[2]; uint16_t s[16]; uint32_t w[8]; } tags;
-    tags.u[0] = tg[0]; tags.u[1] = tg[1];
+    union { uint2 u[4]; uint16_t s[16]; uint32_t w[8]; } tags;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) tags.u[t] = tg[t];
     const float ks = TAIL ? 1.f : ksc;
-    // ---- scores: lane (n, g), element e  <->  token kb * 64 + 16 g + e of column n ----
+    // ---- scores: lane (n, g), element e  <->  token key(e) of column n ----
     float sv[QT][16];
     if (TAIL) {
       floatx4 s[QT][4];
@@ -446,7 +534,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           Frag f, q;
-          f.u = *(const uint4 *)(kt + 4 * t * HD + (c < 2 * KW ? (c >> 1) * 64 + g * 16 + (c & 1) * 8 : KW * 64 + g * 8));
+          f.u = *(const uint4 *)(kt + ((c < 2 * KW ? (c >> 1) * 8 + g * 2 + (c & 1) : KW * 8 + g) * BYTE_BLOCK + 16 * t) * 8);
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) {
             q.u = sm_q[qt][c][lane];
@@ -485,7 +573,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       }
     }
     // whether every column sees the whole block (the same for the whole wave)
-    bool whole_seen = !TAIL && key0 - 16 * g + BYTE_BLOCK <= lim_all;
+    bool whole_seen = !TAIL && kb * BYTE_BLOCK + BYTE_BLOCK <= lim_all;
     if (!TAIL && TG) {
       uint32_t top = 0;
 #pragma unroll
@@ -505,7 +593,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       vref = to;
     }
     if (TAIL && vref == 0.f) vref = 1.f;
-    // (a scale of zero: the sum of the probabilities grows, the outputs do not)
+    // (a scale of zero goes with codes of zero)
     const float ratio = TAIL || vs == 0.f ? 1.f : vs * (1.f / vref), inv_ratio = __builtin_amdgcn_rcpf(ratio);
     Frag ph[QT][2], pl[QT][2];
     float take[QT];
@@ -515,12 +603,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       kf = kf == 0.f ? 1e-37f : kf;                      // (nothing but zeros comes of it, and -infinity stays what it is)
       if (!whole_seen)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sv[qt][e] = ((key0 + e < lim[qt]) & ((int)tags.s[e] <= tag[qt])) ? sv[qt][e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) sv[qt][e] = ((key(e) < lim[qt]) & ((int)tags.s[e] <= tag[qt])) ? sv[qt][e] : -INFINITY;
       float mloc = sv[qt][0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) mloc = fmaxf(mloc, sv[qt][e]);
       mloc = ceilf(fold32(fold16(mloc, Max()), Max()) * kf);
-      const float m_new = fmaxf(m_run[qt], mloc), m_ref = m_new == -INFINITY ? 0.f : m_new;
+      const float m_new = mloc > m_run[qt] + SLACK ? mloc : m_run[qt], m_ref = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = __builtin_amdgcn_exp2f(m_run[qt] - m_ref), down = alpha * grow;
       m_run[qt] = m_new;
       // (fp32 outputs: the scale's logarithm in the exponent would round it by up to 2^-19; NaN has to arrive all the same)
@@ -530,7 +618,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       if (!whole_seen && __any(kf != kf || off != off))  // NaN takes the tokens that are seen only
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          sv[qt][e] = ((key0 + e < lim[qt]) & ((int)tags.s[e] <= tag[qt])) ? sv[qt][e] : -INFINITY;
+          sv[qt][e] = ((key(e) < lim[qt]) & ((int)tags.s[e] <= tag[qt])) ? sv[qt][e] : -INFINITY;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         float p = __builtin_amdgcn_exp2f(sv[qt][e]);
@@ -546,10 +634,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       // (used here: sunk behind the branch below, the first use of the sums stood too close to the product for them to have
       // arrived, where the branch is taken)
       asm volatile("" : "+v"(l_run[qt]), "+v"(take[qt]));
-      if (!TAIL && uniform(vs == 0.f)) {
-        ph[qt][0].u = ph[qt][1].u = make_uint4(0, 0, 0, 0);
-        pl[qt][0].u = pl[qt][1].u = make_uint4(0, 0, 0, 0);
-      }
       if (__any(down != 1.f))
 #pragma unroll
         for (int i = 0; i < NT; ++i) o[qt][i] *= down;
@@ -562,12 +646,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       for (int i = 0; i < NT; ++i) {
         // slots without a token hold anything: zeros instead, so that no product with a zero is NaN
         Frag v0, v1;
-        v0.u = *(const uint4 *)(vt + i * 16 * BYTE_BLOCK);
-        v1.u = *(const uint4 *)(vt + i * 16 * BYTE_BLOCK + 8);
+        v0 = vtail[TAIL ? i : 0][0];
+        v1 = vtail[TAIL ? i : 0][1];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          if (key0 + e >= n_keys) v0.hh[e] = (f16_t)0.f;
-          if (key0 + 8 + e >= n_keys) v1.hh[e] = (f16_t)0.f;
+          if (key(e) >= n_keys) v0.hh[e] = (f16_t)0.f;
+          if (key(8 + e) >= n_keys) v1.hh[e] = (f16_t)0.f;
         }
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
@@ -644,9 +728,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 }
 
 // The splits of a unit become one: a block per (unit, 16-dim tile), wave w takes the splits w, w + 4, ...
-template <typename T, int HD>
+template <typename T, int HD, bool PP>
 __global__ __launch_bounds__(256) void k_byte_merge(ByteAttnArgs a) {
   constexpr int PSTR = HD + 2, NT = HD / 16;
+  constexpr float P_BITS = 15.f - slack_of(PP);
   __shared__ float sm_m[4][64], sm_l[4][64];
   __shared__ floatx4 sm_o[4][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -790,10 +875,7 @@ extern "C" int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, in
   return PD_OK;
 }
 
-// Tiles of 16 columns per work-group: more of them share the conversion of the codes.
-static int byte_tiles(int cols) { return cols > 16 ? 2 : 1; }
-
-struct ByteShape { int qt, nqg, nblk, nsplit; int64_t units, grid; };
+struct ByteShape { int qt, nqg, nblk, nsplit, waves; int64_t units, grid; };
 
 static int byte_shape(const pd_byte_cache *c, int n_head, int n_row, int max_len, ByteShape *out) {
   PD_REQUIRE(n_head >= 1 && n_head % c->n_kv_head == 0, PD_EINVAL, "n_head = %d is no multiple of %d key heads", n_head,
@@ -803,13 +885,12 @@ static int byte_shape(const pd_byte_cache *c, int n_head, int n_row, int max_len
              n_head);
   const int64_t cap = (int64_t)c->n_block * BYTE_BLOCK;
   const int64_t most = max_len ? std::min<int64_t>(max_len, cap) : cap;
-  const int cols = n_row * (n_head / c->n_kv_head);
-  out->qt = byte_tiles(cols);
-  out->nqg = (cols + 16 * out->qt - 1) / (16 * out->qt);
-  out->nblk = (int)((most + BYTE_BLOCK - 1) / BYTE_BLOCK);
   const int64_t heads = (int64_t)c->n_req * c->n_kv_head;
-  out->units = heads * out->nqg;
-  out->nsplit = out->units ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / out->units, out->nblk / 8)) : 1;
+  out->nblk = (int)((most + BYTE_BLOCK - 1) / BYTE_BLOCK);
+  const ByteAttnShape sh = byte_attn_shape(n_row * (n_head / c->n_kv_head), heads, out->nblk);
+  out->qt = sh.tiles; out->waves = sh.waves; out->nsplit = sh.splits;
+  out->nqg = sh.groups;
+  out->units = heads * sh.groups;
   out->grid = (out->nqg > 1 ? (heads + 7) / 8 * 8 * out->nqg : out->units) * out->nsplit;
   return check_grid(std::max(out->grid, out->units * out->qt * (c->head_dim / 16)));
 }
@@ -846,13 +927,15 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
   a.nqg = sh.nqg; a.qt = sh.qt; a.nsplit = sh.nsplit; a.nblk = sh.nblk; a.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t s = (hipStream_t)hip_stream;
   const unsigned grid = (unsigned)sh.grid, tiles = (unsigned)(sh.units * sh.qt * (cache->head_dim / 16));
-#define PD_ATTEND_QT(T, HDV, QT) \
-  hipLaunchKernelGGL((k_byte_attn<T, HDV, !std::is_same<T, bf16_t>::value, QT, 4>), dim3(grid), dim3(256), 0, s, a)
+#define PD_ATTEND_QT(T, HDV, QT, NW) \
+  hipLaunchKernelGGL((k_byte_attn<T, HDV, !std::is_same<T, bf16_t>::value, QT, NW>), dim3(grid), dim3(64 * NW), 0, s, a)
 #define PD_ATTEND(T, HDV)                                                                                    \
   do {                                                                                                       \
-    if (sh.qt == 2) PD_ATTEND_QT(T, HDV, 2);                                                                 \
-    else PD_ATTEND_QT(T, HDV, 1);                                                                            \
-    if (sh.nsplit > 1) hipLaunchKernelGGL((k_byte_merge<T, HDV>), dim3(tiles), dim3(256), 0, s, a);          \
+    if (sh.qt == 2 && sh.waves == 8) PD_ATTEND_QT(T, HDV, 2, 8);                                             \
+    else if (sh.qt == 2) PD_ATTEND_QT(T, HDV, 2, 4);                                                         \
+    else if (sh.waves == 8) PD_ATTEND_QT(T, HDV, 1, 8);                                                      \
+    else PD_ATTEND_QT(T, HDV, 1, 4);                                                                         \
+    if (sh.nsplit > 1) hipLaunchKernelGGL((k_byte_merge<T, HDV, !std::is_same<T, bf16_t>::value>), dim3(tiles), dim3(256), 0, s, a);          \
   } while (0)
   PD_BYTE_TYPES(type, cache->head_dim, PD_ATTEND)
 #undef PD_ATTEND

@@ -41,16 +41,17 @@ def fill(cache, k, v, lens):
 
 
 def check_contents(cache, req, k, v, n):
-    """Codes, scales and tail of one request bit for bit, and what is read."""
+    """Codes, scales and tail of one request bit for bit."""
+    held = cache.to_tensors()
     for name, x in (("k", k), ("v", v)):
         codes, scales, rest, values = u.contents(x[:n])
         whole = n // u.BLOCK
-        got = getattr(cache, name)[req, :, :whole].cpu().numpy()
-        tail = getattr(cache, name + "_tail")[req, :, whole % 2].cpu().numpy()
+        got = held[name][req, :, :whole].cpu().numpy()
+        tail = held[name + "_tail"][req, :, whole % 2].cpu().numpy()
         if name == "v":
             got, tail = got.swapaxes(-1, -2), tail.swapaxes(-1, -2)
         assert np.array_equal(got, codes), name
-        assert np.array_equal(getattr(cache, name + "_scale")[req, :, :whole].cpu().numpy(), scales, equal_nan=True), name
+        assert np.array_equal(held[name + "_scale"][req, :, :whole].cpu().numpy(), scales, equal_nan=True), name
         assert np.array_equal(tail[:, :n % u.BLOCK].view(np.uint16), rest.view(np.uint16)), name
 
 
@@ -394,10 +395,8 @@ def test_offsets_beyond_32_bits():
     from paper_2506_23431_amd import ByteCache
     dim, n_block = 128, 2 ** 19 + 1
     n = n_block * 64 - 30
-    new = lambda *shape, dtype: torch.empty(*shape, dtype=dtype, device=DEV)   # noqa: E731
-    cache = ByteCache.from_tensors(new(1, 1, n_block, 64, dim, dtype=torch.int8), new(1, 1, n_block, dim, 64, dtype=torch.int8),
-                                   new(1, 1, n_block, dtype=torch.float32).fill_(1), new(1, 1, n_block, dtype=torch.float32).fill_(1),
-                                   new(1, 1, 2, 64, dim, dtype=torch.float16), new(1, 1, 2, dim, 64, dtype=torch.float16))
+    cache = ByteCache(1, 1, dim, n_block * 64, device=DEV)
+    cache.k_scale.fill_(1), cache.v_scale.fill_(1)
     k, kn = data(71, 1, 300, 1, dim, "f32")
     v, vn = data(72, 1, 300, 1, dim, "f32")
     cache.append(k[:, :64], v[:, :64], ints([64]))
@@ -421,6 +420,32 @@ def test_offsets_beyond_32_bits():
     assert (np.abs(out[0].cpu().numpy() - want) <= tol).all()
 
 
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+def test_plain_tensors_go_in_and_come_out(dim):
+    """A cache made from plain codes reads as code times scale, and gives the same tensors back."""
+    from paper_2506_23431_amd import ByteCache
+    rng = np.random.default_rng(dim)
+    plain = {"k": rng.integers(-127, 128, (2, 3, 4, 64, dim)).astype(np.int8),
+             "v": rng.integers(-127, 128, (2, 3, 4, dim, 64)).astype(np.int8),
+             "k_scale": rng.random((2, 3, 4)).astype(np.float32), "v_scale": rng.random((2, 3, 4)).astype(np.float32),
+             "k_tail": rng.standard_normal((2, 3, 2, 64, dim)).astype(np.float16),
+             "v_tail": rng.standard_normal((2, 3, 2, dim, 64)).astype(np.float16)}
+    cache = ByteCache.from_tensors(**{n: torch.from_numpy(x).to(DEV) for n, x in plain.items()})
+    for n, t in cache.to_tensors().items():
+        assert np.array_equal(t.cpu().numpy(), plain[n]), n
+    lens = [200, 129]
+    k, v = cache.read(ints(lens), 200)
+    for r, n in enumerate(lens):
+        whole = n // 64
+        want_k = (plain["k"][r].astype(np.float32) * plain["k_scale"][r][..., None, None]).astype(np.float32)
+        want_v = (plain["v"][r].astype(np.float32) * plain["v_scale"][r][..., None, None]).astype(np.float32).swapaxes(-1, -2)
+        for got, want, tail in ((k, want_k, plain["k_tail"][r, :, whole % 2]),
+                                (v, want_v, plain["v_tail"][r, :, whole % 2].swapaxes(-1, -2))):
+            flat = np.concatenate([want[:, :whole].reshape(3, whole * 64, dim), tail[:, :n - whole * 64].astype(np.float32)], axis=1)
+            assert np.array_equal(got[r, :n].cpu().numpy(), flat.transpose(1, 0, 2))
+            assert (got[r, n:] == 0).all()
+
+
 def test_refusals_of_the_binding():
     from paper_2506_23431_amd import ByteCache, PdError
     cache = cache_of(2, 2, 64, 128)
@@ -437,8 +462,11 @@ def test_refusals_of_the_binding():
                  lambda: cache.attention(k, lens, row_limit=lens), lambda: cache.attention(k, lens, scale=float("nan")),
                  lambda: cache.attention(k, lens, scale=float("inf")), lambda: cache.attention(k, lens, max_len=-1),
                  lambda: cache.attention(k[..., :32], lens), lambda: cache.attention(k.cpu(), lens),
-                 lambda: ByteCache(1, 1, 48, 64), lambda: ByteCache.from_tensors(cache.k, cache.v[:, :1], cache.k_scale, cache.v_scale, cache.k_tail, cache.v_tail),
-                 lambda: ByteCache.from_tensors(*(t.cpu() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.k_tail, cache.v_tail)))):
+                 lambda: ByteCache(1, 1, 48, 64), lambda: ByteCache(0, 1, 64, 64), lambda: ByteCache(1, 1, 64, 0),
+                 lambda: ByteCache(1, 1, 64, 64, device="cpu"),
+                 lambda: ByteCache.from_tensors(**{**cache.to_tensors(), "v": cache.v}),
+                 lambda: ByteCache.from_tensors(**{**cache.to_tensors(), "k_scale": cache.k_scale.half()}),
+                 lambda: ByteCache.from_tensors(**{n: t.cpu() for n, t in cache.to_tensors().items()})):
         with pytest.raises(PdError):
             call()
     # no rows, no tokens: nothing to do
