@@ -404,9 +404,12 @@ int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, int n_tok, co
  *   out_lse    fp32 [n_req][n_row][n_head] or NULL: log(sum_j exp(scale q.k_j)), -infinity for a row that sees nothing
  *   workspace  at least pd_byte_attention_workspace_bytes (same arguments; 0: they are invalid), 16-byte aligned; it holds
  *              nothing between calls, and calls that may overlap need one each
- * Codes enter the products exactly; 16-bit queries too, but for parts 2^24 times smaller than the row's largest.  Probabilities are
- * rounded to halves (relative 2^-12; fp32 and half queries: pairs of halves, 2^-23), sums and the running maximum are fp32.  Infinities and NaN
- * in tokens that a row does not see do not reach it, save that a NaN reaches every row that sees any token of its block. */
+ * Scores are products of whole numbers, exact: codes as they are, queries in steps of the row's largest / 32512 (bf16) or of at
+ * most its 2^-21 (fp32, half), so at most half of that off; against the tail's halves, queries are halves (fp32: pairs of them).
+ * Probabilities are rounded to halves (relative 2^-12; fp32 and half queries: pairs of halves, 2^-22; parts below 2^-35 of the
+ * row's largest get lost), and so counted in out_lse; sums and the running maximum are fp32.  Infinities and NaN in tokens that a
+ * row does not see do not reach it, save that a NaN reaches every row that sees any token of its block; of a query, they reach
+ * its own row. */
 size_t pd_byte_attention_workspace_bytes(const pd_byte_cache *cache, int n_head, int n_row, int max_len);
 int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const int64_t *q_strides, int n_head, int n_row,
                       const int32_t *lens, const int32_t *row_limit, const uint16_t *key_tag, const int32_t *row_tag,

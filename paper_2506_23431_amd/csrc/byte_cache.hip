@@ -271,7 +271,7 @@ struct ByteAttnArgs {
   float *lse;                         // [req][row][head] or NULL
   float *part;
   int n_row, group, nqg, qt, nsplit, nblk; // group: query heads per key head; nqg: groups of 16 qt (row, query head) columns
-  float scale_log2;
+  float scale_log2, scale_low;             // log2(e) times the scale, and what its rounding left
 };
 
 // Four codes as four halves, exactly: a byte with its sign bit turned is code + 128, under 0x64 it is the half 1024 + 128 +
@@ -321,7 +321,8 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 // out of the matrix instruction with a lane holding 16 tokens of one column, which are its operand for the outputs as they are:
 // element e of step s of group g is token 32 s + 16 (e >> 2) + 4 g + (e & 3) of the block.
 //  * Scores are products of bytes, exact in 32-bit integers: the keys' codes as they lie, queries as whole numbers of two bytes
-//    (bf16) or three (fp32, half), steps of the row's largest / 32512 or / 2^23.  No key is converted.
+//    (bf16) or three (fp32, half), in steps of the row's largest / 32512 or of a power of two at most 2^-21 of it.  No key is
+//    converted.
 //  * Values become halves in registers, exactly, once for QT tiles of 16 columns.
 //  * A block's key scale multiplies its scores.  The reference of the exponentials is a whole number (a running maximum rounded
 //    up), so that taking it off rounds nothing and rescaling by its change is exact.
@@ -436,12 +437,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       const bool finite = top < 0x7f800000u;
       const int ex = finite ? max((int)(top >> 23) - 127, -100) : 8;
       const float down = __uint_as_float((uint32_t)(127 + 8 - ex) << 23);
-      // whole numbers up to 127 in their highest byte; the factor of a row that is not finite is NaN, and so are its scores
-      constexpr float MOST = NP == 2 ? 127.f * 256.f : 127.f * 65536.f;
+      // whole numbers up to 127 in their highest byte: two bytes as finely as they go, three by a power of two, which rounds
+      // nothing; the factor of a row that is not finite is NaN, and so are its scores
       const float big = fmaxf(__uint_as_float(top), 1e-31f), sign = a.scale_log2 < 0.f ? -1.f : 1.f;   // (factors are not negative)
-      const float up = finite ? MOST / big * sign : 0.f;
+      const float most = NP == 2 ? 127.f * 256.f / big : __uint_as_float((uint32_t)(127 + 21 - ex) << 23);
+      const float up = finite ? most * sign : 0.f;
       if (pt == 0) {
-        sm_qf[qt][0][m] = finite ? big / MOST * fabsf(a.scale_log2) : __uint_as_float(0x7fc00000u);
+        sm_qf[qt][0][m] = !finite ? __uint_as_float(0x7fc00000u)
+                          : NP == 2 ? big / (127.f * 256.f) * fabsf(a.scale_log2) : __uint_as_float((uint32_t)(127 - 21 + ex) << 23);
         sm_qf[qt][1][m] = __uint_as_float((uint32_t)(127 - 8 + ex) << 23) * fabsf(a.scale_log2);
       }
 #pragma unroll
@@ -599,7 +602,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     float take[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-      float kf = TAIL ? sm_qf[qt][1][n] : qf[qt] * ks;
+      // fp32: the factor with what its roundings leave, which would shift a block's probabilities together
+      float kf = TAIL ? sm_qf[qt][1][n] : qf[qt] * ks, kf_low = 0.f;
+      if (!TAIL && NP == 3) {
+        const float f = qf[qt] * fabsf(a.scale_log2);
+        kf = f * ks;
+        if (sizeof(T) == 4) kf_low = fmaf(qf[qt] * a.scale_low, ks, fmaf(f, ks, -kf));
+      }
       kf = kf == 0.f ? 1e-37f : kf;                      // (nothing but zeros comes of it, and -infinity stays what it is)
       if (!whole_seen)
 #pragma unroll
@@ -614,7 +623,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       // (fp32 outputs: the scale's logarithm in the exponent would round it by up to 2^-19; NaN has to arrive all the same)
       const float off = P_BITS - m_ref + (sizeof(T) == 2 ? lg2(ratio) : 0.f * ratio);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sv[qt][e] = fmaf(sv[qt][e], kf, off);
+      for (int e = 0; e < 16; ++e) {
+        const float x = fmaf(sv[qt][e], kf, off);
+        sv[qt][e] = sizeof(T) == 4 && !TAIL ? fmaf(fmaxf(sv[qt][e], -3e38f), kf_low, x) : x;
+      }
       if (!whole_seen && __any(kf != kf || off != off))  // NaN takes the tokens that are seen only
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -915,7 +927,7 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
   PD_REQUIRE(((uintptr_t)out & 15) == 0, PD_EINVAL, "out must be 16-byte aligned");
   const int es = type_bytes(type);
   PD_REQUIRE(((uintptr_t)q & (es - 1)) == 0, PD_EINVAL, "q must be aligned to its type");
-  PD_REQUIRE(scale == scale && std::abs(scale) <= 3.0e38f, PD_EINVAL, "scale must be a finite number");
+  PD_REQUIRE(scale == scale && std::abs(scale) <= 2.0e38f, PD_EINVAL, "scale must be a number of magnitude up to 2e38");
   const size_t need = pd_byte_attention_workspace_bytes(cache, n_head, n_row, max_len);
   PD_REQUIRE(sh.nsplit == 1 || (workspace && workspace_bytes >= need), PD_ENOMEM, "workspace too small: %zu bytes given, %zu needed",
              workspace ? workspace_bytes : (size_t)0, need);
@@ -924,7 +936,9 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
   a.c = view(cache); a.q = q; a.q_req = q_strides[0]; a.q_row = q_strides[1]; a.q_head = q_strides[2];
   a.lens = lens; a.row_limit = row_limit; a.key_tag = key_tag; a.row_tag = row_tag; a.out = out; a.lse = out_lse;
   a.part = (float *)workspace; a.n_row = n_row; a.group = n_head / cache->n_kv_head;
-  a.nqg = sh.nqg; a.qt = sh.qt; a.nsplit = sh.nsplit; a.nblk = sh.nblk; a.scale_log2 = scale * 1.4426950408889634f;
+  a.nqg = sh.nqg; a.qt = sh.qt; a.nsplit = sh.nsplit; a.nblk = sh.nblk; 
+  a.scale_log2 = (float)(scale * 1.4426950408889634);
+  a.scale_low = (float)(std::abs(scale * 1.4426950408889634) - std::abs((double)a.scale_log2));
   hipStream_t s = (hipStream_t)hip_stream;
   const unsigned grid = (unsigned)sh.grid, tiles = (unsigned)(sh.units * sh.qt * (cache->head_dim / 16));
 #define PD_ATTEND_QT(T, HDV, QT, NW) \

@@ -72,20 +72,21 @@ SMALLEST = {"f32": 2.0 ** -150, "bf16": 2.0 ** -134, "f16": 2.0 ** -25}        #
 def tolerance(kind, out, mag, scores, dim, tokens, largest):
     """Largest error of (out, lse), from the roundings of the definition's steps.
 
-    A score: queries are whole numbers of steps of the row's largest / 32512 (bf16) or / 127 2^16 (fp32, half), half a step off;
+    A score: queries are whole numbers of steps of the row's largest / 32512 (bf16) or at most its 2^-21 (fp32, half), half a step off;
     against the tail they are halves (11 bits hold a 16-bit query but for parts below 2^-24 of the row's largest) or pairs.
     Products with codes are exact; those with the tail's halves are added in fp32 in up to two passes, each addition off by
     2^-24 of what the magnitudes sum up to; three factors in fp32.  A probability: its score's error, the exponential (2^-22),
     and as an operand 2^-12 (bf16 queries) or 2^-22, but never nearer than half of the smallest half, 2^-25, where the row's
-    largest is between 2^14 and 2^15: 2^-39 of it, times 2 where the value scale is that much below its power of two (2^12 at
-    most), times the values' largest magnitude for each token (the largest probability alone makes the sum that divides).  The
-    sums are of the probabilities as they enter the products.  Sums over the tokens in fp32: 2^-24 each at most.  Then the
-    output's own rounding, by half of its smallest number at least."""
+    largest is at least 2^11 (pairs: 2^7 for single halves) over 2 (the reference is rounded up), times 1/2 to 1 for the value scale
+    over its power of two (2^-12 where scales differ that much): 2^-35 of it for pairs, 2^-31 for single halves, times the values'
+    largest magnitude for each token (the largest probability alone makes the sum that divides).  The sums are of the
+    probabilities as they enter the products.  Sums over the tokens in fp32: 2^-24 each at most.  Then the output's own
+    rounding, by half of its smallest number at least."""
     dot, top, flat = scores
-    step = 1 / 65024 if kind == "bf16" else 2.0 ** -23.9
+    step = 1 / 65024 if kind == "bf16" else 2.0 ** -22
     score = dot * ((2 * dim + 8) * 2.0 ** -24 + 2.0 ** -22) + flat * (step + 2.0 ** -24) + top * 2.0 ** -22
     prob = score + 2.0 ** -22 + (2.0 ** -12 if kind == "bf16" else 2.0 ** -22)
     rel = 2 * prob + 2 * (tokens + 64) * 2.0 ** -24
     lse = prob + (tokens + 64) * 2.0 ** -24
     rounded = np.maximum(np.abs(out) * HALF_STEP[kind], SMALLEST[kind])
-    return mag * rel[..., None] * 1.01 + rounded + tokens * largest * 2.0 ** -38 + 1e-30, lse + (top + 16) * 2.0 ** -23
+    return mag * rel[..., None] * 1.01 + rounded + tokens * largest * 2.0 ** (-31 if kind == "bf16" else -35) + 1e-30, lse + (top + 16) * 2.0 ** -23
