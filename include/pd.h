@@ -327,6 +327,8 @@ int pd_measure_read_bandwidth(const void *dev_buf, size_t buf_bytes, size_t chun
  *   PD_INFO_STREAM_LOADS    1, 2: decode steps use the non-temporal hint (the value of PD_OPT_STREAM_LOADS)
  *   PD_INFO_KEPT_BYTES      bytes of the weights of a decode step that keep ordinary loads while the others take the
  *                           hint (at most 210 MB; 0 without the hint)
+ *   PD_INFO_BYTE_BLOCKS     blocks of 64 tokens of every request's context that decode steps read from 8-bit codes
+ *                           (pd_byte_context; 0: none)
  *   PD_INFO_KV_SATURATED    keys and values written since pd_create whose magnitude exceeded the
  *                           largest half (65504) and were stored as +-65504 (dtype 1 only; always
  *                           0 for dtype 0).  Non-zero means the 16-bit cache cannot represent
@@ -338,6 +340,7 @@ int pd_measure_read_bandwidth(const void *dev_buf, size_t buf_bytes, size_t chun
 #define PD_INFO_CONTEXT_PAIRS  4
 #define PD_INFO_STREAM_LOADS   5
 #define PD_INFO_KEPT_BYTES     6
+#define PD_INFO_BYTE_BLOCKS    7
 int pd_get_info(pd_ctx *ctx, int key, void *hip_stream, int64_t *value);
 
 /* ---- operators over a cache of keys and values held in 8 bits -------------------------------------------------------
@@ -415,6 +418,19 @@ int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const
                       const int32_t *lens, const int32_t *row_limit, const uint16_t *key_tag, const int32_t *row_tag,
                       float scale, int max_len, void *out, float *out_lse, void *workspace, size_t workspace_bytes,
                       void *hip_stream);
+
+/* A decoder's context in 8 bits: from now on the decode steps of `ctx` (decoder-only form, matrix-core kernels) read the whole
+ * blocks of 64 tokens of every request's context from codes as above, one scale per block, layer and head, and everything behind
+ * them (the rest of the context and all generated tokens) from the 16-bit cache, which the context pass and pd_teacher_forced
+ * go on using for all of it: half of the bytes of the attention's hot loop for a further buffer.  Layers that keep pairs of halves
+ * (kv_pair_layers) stay as they are.  A caller's trade, not the library's: keys and values of the context are off by up to half
+ * a scale, 1/254 of their block's largest (measured beside the other switches in PD_OPT_CONTEXT_SPLIT_ACT's terms: BYTE_FIGURES).
+ *   dev_buffer  DEVICE, 256-byte aligned, at least pd_byte_context_bytes(ctx) (0: this context cannot have one), to outlive the
+ *               ctx or the next such call; NULL: back to the 16-bit cache
+ * Contexts that are encoded already get their codes at once, others at the end of pd_prefill_context; asynchronous on
+ * hip_stream.  PD_OPT_PROFILE 1 and 2 bracket the kernel, and the pair, with events recorded beside them; 3 has no effect on it. */
+size_t pd_byte_context_bytes(const pd_ctx *ctx);
+int pd_byte_context(pd_ctx *ctx, void *dev_buffer, size_t bytes, void *hip_stream);
 
 /* Message for the last error on this thread (static storage, never NULL). */
 const char *pd_last_error(void);

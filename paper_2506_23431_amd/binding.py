@@ -20,11 +20,13 @@ PD_OPT_CONTEXT_ATTN = 9
 PD_INFO_KERNEL_PATH, PD_INFO_KV_PAIR_LAYERS, PD_INFO_KV_SATURATED, PD_INFO_CONTEXT_PAIRS = 1, 2, 3, 4
 PD_INFO_STREAM_LOADS = 5
 PD_INFO_KEPT_BYTES = 6
+PD_INFO_BYTE_BLOCKS = 7
 
 EXPORTS = ["pd_workspace_bytes", "pd_create", "pd_destroy", "pd_prefill_context", "pd_decode_step",
            "pd_generate", "pd_generate_static", "pd_decode_steps", "pd_reset_decode", "pd_set_option", "pd_profile_read",
            "pd_measure_read_bandwidth", "pd_get_info", "pd_last_error", "pd_encdec_workspace_bytes", "pd_encdec_create", "pd_teacher_forced",
-           "pd_byte_append", "pd_byte_read", "pd_byte_attention_workspace_bytes", "pd_byte_attention"]
+           "pd_byte_append", "pd_byte_read", "pd_byte_attention_workspace_bytes", "pd_byte_attention",
+           "pd_byte_context_bytes", "pd_byte_context"]
 
 
 class PdError(RuntimeError):
@@ -111,6 +113,9 @@ def load():
     lib.pd_byte_attention_workspace_bytes.argtypes = [cache, C.c_int, C.c_int, C.c_int]
     lib.pd_byte_attention.argtypes = [cache, vp, C.c_int, i64p, C.c_int, C.c_int, vp, vp, vp, vp, C.c_float, C.c_int, vp, vp,
                                       vp, sz, vp]
+    lib.pd_byte_context_bytes.restype = sz
+    lib.pd_byte_context_bytes.argtypes = [vp]
+    lib.pd_byte_context.argtypes = [vp, vp, sz, vp]
     for name in EXPORTS:
         getattr(lib, name)
     _lib = lib
@@ -287,6 +292,21 @@ class PipelinedDecoder:
 
     def set_option(self, key, value):
         _check(self.lib.pd_set_option(self.ctx, key, value))
+
+    def use_byte_context(self, on=True):
+        """pd_byte_context: decode steps read the whole blocks of 64 tokens of the contexts from 8-bit codes (a buffer of this
+        object's holds them); False: back to the 16-bit cache."""
+        buffer, base, nbytes = None, None, 0
+        if on:
+            nbytes = self.lib.pd_byte_context_bytes(self.ctx)
+            if nbytes == 0:
+                raise PdError("an 8-bit context needs a decoder-only configuration on the matrix-core kernels")
+            buffer = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
+            base = C.c_void_p((buffer.data_ptr() + 255) // 256 * 256)
+        else:
+            self.torch.cuda.synchronize(self.device)          # (steps under way may still read the codes)
+        _check(self.lib.pd_byte_context(self.ctx, base, nbytes, self._stream()))
+        self._byte_buffer = buffer
 
     def get_info(self, key):
         v = C.c_int64(0)

@@ -525,6 +525,39 @@ int mfma_attention(pd_ctx *c, const LayerPtrs &lw, int A, int nreq, int req0, in
     int rc = mfma_attention_ctx(c, lw, A, nreq, req0, kv_override, s);
     if (rc != 1) return rc;
   }
+  if (kv_override < 0 && !mode && lw.b_k && c->L >= PD_BYTE_BLOCK) {      // decode step over a context in 8 bits
+    const bool timed = c->opt_profile == 1 || c->opt_profile == 2;
+    if (timed) {
+      while (c->ev_pool.size() < c->ev_used + 2) {
+        hipEvent_t ev;
+        PD_CHECK_HIP(hipEventCreate(&ev));
+        c->ev_pool.push_back(ev);
+      }
+      PD_CHECK_HIP(hipEventRecord(c->ev_pool[c->ev_used], s));
+    }
+    int splits = 1;
+    int rc = byte_context_attention(c, lw, A, nreq, req0, s, &splits);
+    if (rc) return rc;
+    if (timed && c->opt_profile == 1) PD_CHECK_HIP(hipEventRecord(c->ev_pool[c->ev_used + 1], s));
+    if (splits > 1) {
+      const int units = nreq * ((A + 15) / 16) * g.n_head;
+      bf16_t *lo = mfma_lo(c, c->att, g.d_model);
+#define PD_MERGE(HDV) hipLaunchKernelGGL(k_attn_merge<HDV>, dim3(units, HDV / 16), dim3(256), 0, s, c->att_part, c->rows.flags, (bf16_t *)c->att, lo, heads_rows(g.n_head, A), splits)
+      switch (g.head_dim) {
+        case 32: PD_MERGE(32); break;
+        case 64: PD_MERGE(64); break;
+        case 96: PD_MERGE(96); break;
+        default: PD_MERGE(128); break;
+      }
+#undef PD_MERGE
+      PD_CHECK_HIP(hipGetLastError());
+    }
+    if (timed) {
+      if (c->opt_profile == 2) PD_CHECK_HIP(hipEventRecord(c->ev_pool[c->ev_used + 1], s));
+      c->ev_used += 2;
+    }
+    return PD_OK;
+  }
   AttnArgs a;
   memset(&a, 0, sizeof(a));
   a.q = (const f16_t *)c->q; a.q_lo = (const f16_t *)mfma_lo(c, c->q, g.d_model);

@@ -26,36 +26,95 @@ struct StoreArgs {
   int n_new, span;                    // most new tokens; blocks that they can touch
 };
 
-// NaN stays, everything else beyond the halves saturates
-__device__ __forceinline__ f16_t to_half(float x) { return x != x ? (f16_t)x : f32_to_f16_sat(x); }
-
-// The whole number nearest to x / s, ties to even, exactly: the product with the reciprocal is at most one off, and the
-// remainder, a whole multiple of the scale's last bit below 2^24 of them, is computed without rounding.
-__device__ __forceinline__ int code_of(float x, float s, float inv) {
-  float q = rintf(x * inv);
-  const float r = fmaf(-q, s, x), h = 0.5f * s;
-  const bool odd = ((int)q & 1) != 0;
-  q += (r > h || (r == h && odd)) ? 1.f : (r < -h || (r == -h && odd)) ? -1.f : 0.f;
-  return (int)fminf(fmaxf(q, -127.f), 127.f);
+// Codes of N halves: the whole numbers nearest to x / s, ties to even, exactly.  The product with the reciprocal is at most one
+// off, and the remainder, a whole multiple of the scale's last bit below 2^24 of them, is computed without rounding: below half
+// a scale it proves the number; else (next to a border between two, about one in 10^5) the neighbours are compared.
+template <int N>
+__device__ __forceinline__ void codes_of(const f16_t *x, float s, float inv, int *c) {
+  float worst = 0.f;
+  const float h = 0.5f * s;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float q = rintf((float)x[j] * inv);
+    worst = fmaxf(worst, fabsf(fmaf(-q, s, (float)x[j])));
+    c[j] = (int)q;
+  }
+  if (worst >= h)
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float r = fmaf(-(float)c[j], s, (float)x[j]);
+      const bool odd = (c[j] & 1) != 0;
+      c[j] += (r > h || (r == h && odd)) ? 1 : (r < -h || (r == -h && odd)) ? -1 : 0;
+      c[j] = min(max(c[j], -127), 127);
+    }
 }
+__device__ __forceinline__ uint32_t magnitude(f16_t x) { return __builtin_bit_cast(uint16_t, x) & 0x7fffu; }
 
 __device__ __forceinline__ uint32_t bytes4(int a, int b, int c, int d) {
   const uint32_t lo = __builtin_amdgcn_perm((uint32_t)b, (uint32_t)a, 0x0c0c0400u), hi = __builtin_amdgcn_perm((uint32_t)d, (uint32_t)c, 0x04000c0cu);
   return lo | hi;
 }
 
+// A whole block, by tokens in LDS (P halves a row), and each thread's largest magnitude: codes and scale.
+template <int HD, int P>
+__device__ __forceinline__ void seal_block(const f16_t *tile, uint32_t *sm_top, uint32_t top, int kind, const ByteCache &cache, size_t block) {
+  const int tid = threadIdx.x;
+  // the largest magnitude by its bits, where NaN is above everything: then the scale is NaN, and so is the block
+  for (int m = 32; m; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+  if ((tid & 63) == 0) sm_top[tid >> 6] = top;
+  __syncthreads();
+  top = max(max(sm_top[0], sm_top[1]), max(sm_top[2], sm_top[3]));
+  const float scale = __fdiv_rn((float)__builtin_bit_cast(f16_t, (uint16_t)top), 127.f);
+  const float inv = 1.f / scale;
+  if (tid == 0) (kind ? cache.v_scale : cache.k_scale)[block] = scale;
+  int8_t *dst = (kind ? cache.v : cache.k) + block * BYTE_BLOCK * HD;
+  if (!(scale > 0.f)) {                                // zeros, or a NaN among them: codes of zero
+    for (int e = tid; e < BYTE_BLOCK * HD / 16; e += 256) ((uint4 *)dst)[e] = make_uint4(0, 0, 0, 0);
+  } else if (!kind) {
+    for (int e = tid; e < BYTE_BLOCK * HD / 16; e += 256) {        // 16 dims of a token
+      union { uint4 q[2]; f16_t h[16]; } y;
+      const f16_t *row = &tile[(e & 63) * P + (e >> 6) * 16];
+      y.q[0] = *(const uint4 *)row; y.q[1] = *(const uint4 *)(row + 8);
+      int c[16];
+      codes_of<16>(y.h, scale, inv, c);
+      ((uint4 *)dst)[e] = make_uint4(bytes4(c[0], c[1], c[2], c[3]), bytes4(c[4], c[5], c[6], c[7]),
+                                     bytes4(c[8], c[9], c[10], c[11]), bytes4(c[12], c[13], c[14], c[15]));
+    }
+  } else {
+    for (int e = tid; e < BYTE_BLOCK * HD / 32; e += 256) {        // 8 places of 4 dims
+      const int half = e & 1, d = (e >> 1) % (HD / 4) * 4, g = (e >> 1) / (HD / 4);
+      f16_t x4[4][8];
+      int c[4][8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        union { uint2 q; f16_t h[4]; } z;
+        z.q = *(const uint2 *)&tile[(16 * (2 * half + (j >> 2)) + 4 * g + (j & 3)) * P + d];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x4[i][j] = z.h[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) codes_of<8>(x4[i], scale, inv, c[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(uint2 *)(dst + (g * HD + d + i) * 16 + half * 8) =
+            make_uint2(bytes4(c[i][0], c[i][1], c[i][2], c[i][3]), bytes4(c[i][4], c[i][5], c[i][6], c[i][7]));
+    }
+  }
+}
+
 // One work-group per (request, head, touched block, keys or values): the block's tokens go to LDS as halves, the old ones from
 // the tail, the new ones from the caller (all requested before the first is used); a whole block leaves as codes, one that is not
 // yet whole as halves of its new tokens.  Bound by the bytes.
 template <typename T, int HD, bool WIDE>
-__global__ __launch_bounds__(256) void k_byte_store(StoreArgs a) {
+__global__ __launch_bounds__(256, 3) void k_byte_store(StoreArgs a) {
   constexpr int P = HD + 8;                              // halves per token row in LDS (16-byte rows)
   constexpr int IT = HD / 32;                            // pieces of 8 dims per thread
   __shared__ f16_t tile[BYTE_BLOCK * P];
   __shared__ uint32_t sm_top[4];
   const int tid = threadIdx.x;
-  const int kind = blockIdx.x & 1, u = blockIdx.x >> 1;
-  const int i0 = u % a.span, rh = u / a.span, h = rh % a.c.n_kv_head, req = rh / a.c.n_kv_head;
+  int u = blockIdx.x;                                    // heads first: their rows lie together
+  const int h = u % a.c.n_kv_head; u /= a.c.n_kv_head;
+  const int kind = u & 1, i0 = (u >> 1) % a.span, req = (u >> 1) / a.span;
   const int count = a.counts ? a.counts[req] : a.n_new, len = a.lens[req], before = len - count;
   if (count <= 0 || count > a.n_new || before < 0 || (int64_t)len > (int64_t)a.c.n_block * BYTE_BLOCK) return;
   const int first = before / BYTE_BLOCK, last = (len - 1) / BYTE_BLOCK;      // touched blocks
@@ -85,21 +144,36 @@ __global__ __launch_bounds__(256) void k_byte_store(StoreArgs a) {
 #pragma unroll
       for (int it = 0; it < IT; ++it) old[it] = ((const uint4 *)tail)[tid + it * 256];
     uint32_t top = 0;
+    union Eight { f16_t h[8]; uint4 q; } y[IT];
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int t = (tid + it * 256) / (HD / 8);
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { y[it].h[j] = (f16_t)x[it][j]; m = max(m, magnitude(y[it].h[j])); }
+      top = max(top, t < n_old || t >= n_all ? 0u : m);
+    }
+    if (top >= 0x7c00u) {                                // beyond the halves: saturated; NaN stays
+      top = 0;
+#pragma unroll
+      for (int it = 0; it < IT; ++it) {
+        const int t = (tid + it * 256) / (HD / 8);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (magnitude(y[it].h[j]) == 0x7c00u) y[it].h[j] = (f16_t)(x[it][j] > 0.f ? 65504.f : -65504.f);
+          if (t >= n_old && t < n_all) top = max(top, magnitude(y[it].h[j]));
+        }
+      }
+    }
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
       const int e = tid + it * 256, t = e / (HD / 8), d = e % (HD / 8) * 8;
       if (t < n_old || t >= n_all) continue;
-      union { f16_t h[8]; uint4 q; } y;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        y.h[j] = to_half(x[it][j]);
-        top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y.h[j]) & 0x7fff));
-      }
-      if (whole) *(uint4 *)&tile[t * P + d] = y.q;
-      else if (!kind) *(uint4 *)(tail + ((d >> 3) * BYTE_BLOCK + t) * 8) = y.q;
+      if (whole) *(uint4 *)&tile[t * P + d] = y[it].q;
+      else if (!kind) *(uint4 *)(tail + ((d >> 3) * BYTE_BLOCK + t) * 8) = y[it].q;
       else
 #pragma unroll
-        for (int j = 0; j < 8; ++j) tail[(((t >> 5) * 4 + ((t >> 2) & 3)) * HD + d + j) * 8 + ((t >> 4) & 1) * 4 + (t & 3)] = y.h[j];
+        for (int j = 0; j < 8; ++j) tail[(((t >> 5) * 4 + ((t >> 2) & 3)) * HD + d + j) * 8 + ((t >> 4) & 1) * 4 + (t & 3)] = y[it].h[j];
     }
     if (!whole) continue;
     if (mixed) {                                         // ... and the ones that were in the tail
@@ -113,7 +187,7 @@ __global__ __launch_bounds__(256) void k_byte_store(StoreArgs a) {
           if (t >= n_old) continue;
           *(uint4 *)&tile[t * P + d] = y.q;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y.h[j]) & 0x7fff));
+          for (int j = 0; j < 8; ++j) top = max(top, magnitude(y.h[j]));
         } else {
           const int d = e % HD, sg = e / HD;
 #pragma unroll
@@ -121,49 +195,12 @@ __global__ __launch_bounds__(256) void k_byte_store(StoreArgs a) {
             const int t = 16 * (2 * (sg >> 2) + (j >> 2)) + 4 * (sg & 3) + (j & 3);
             if (t >= n_old) continue;
             tile[t * P + d] = y.h[j];
-            top = max(top, (uint32_t)(__builtin_bit_cast(uint16_t, y.h[j]) & 0x7fff));
+            top = max(top, magnitude(y.h[j]));
           }
         }
       }
     }
-    // the largest magnitude by its bits, where NaN is above everything: then the scale is NaN, and so is the block
-    for (int m = 32; m; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
-    if ((tid & 63) == 0) sm_top[tid >> 6] = top;
-    __syncthreads();
-    top = max(max(sm_top[0], sm_top[1]), max(sm_top[2], sm_top[3]));
-    const float scale = __fdiv_rn((float)__builtin_bit_cast(f16_t, (uint16_t)top), 127.f);
-    const bool some = scale > 0.f;                       // (zeros, and NaN: codes of zero)
-    const float inv = some ? 1.f / scale : 0.f, sc = some ? scale : 1.f;
-    if (tid == 0) (kind ? a.c.v_scale : a.c.k_scale)[rhz * a.c.n_block + b] = scale;
-    int8_t *dst = (kind ? a.c.v : a.c.k) + (rhz * a.c.n_block + b) * BYTE_BLOCK * HD;
-    if (!kind) {
-      for (int e = tid; e < BYTE_BLOCK * HD / 16; e += 256) {        // 16 dims of a token
-        union { uint4 q[2]; f16_t h[16]; } y;
-        const f16_t *row = &tile[(e & 63) * P + (e >> 6) * 16];
-        y.q[0] = *(const uint4 *)row; y.q[1] = *(const uint4 *)(row + 8);
-        int c[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) c[j] = some ? code_of((float)y.h[j], sc, inv) : 0;
-        ((uint4 *)dst)[e] = make_uint4(bytes4(c[0], c[1], c[2], c[3]), bytes4(c[4], c[5], c[6], c[7]),
-                                       bytes4(c[8], c[9], c[10], c[11]), bytes4(c[12], c[13], c[14], c[15]));
-      }
-    } else {
-      for (int e = tid; e < BYTE_BLOCK * HD / 32; e += 256) {        // 8 places of 4 dims
-        const int half = e & 1, d = (e >> 1) % (HD / 4) * 4, g = (e >> 1) / (HD / 4);
-        int c[4][8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          union { uint2 q; f16_t h[4]; } y;
-          y.q = *(const uint2 *)&tile[(16 * (2 * half + (j >> 2)) + 4 * g + (j & 3)) * P + d];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) c[i][j] = some ? code_of((float)y.h[i], sc, inv) : 0;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *(uint2 *)(dst + (g * HD + d + i) * 16 + half * 8) =
-              make_uint2(bytes4(c[i][0], c[i][1], c[i][2], c[i][3]), bytes4(c[i][4], c[i][5], c[i][6], c[i][7]));
-      }
-    }
+    seal_block<HD, P>(tile, sm_top, top, kind, a.c, rhz * a.c.n_block + b);
   }
 }
 
@@ -186,8 +223,9 @@ __global__ __launch_bounds__(256) void k_byte_read(ReadArgs a) {
   f16_t *tile = (f16_t *)mem;
   int8_t *codes = (int8_t *)mem;
   const int tid = threadIdx.x;
-  const int kind = blockIdx.x & 1, u = blockIdx.x >> 1;
-  const int i0 = u % a.span, rh = u / a.span, h = rh % a.c.n_kv_head, req = rh / a.c.n_kv_head;
+  int u = blockIdx.x;                                    // heads first: their rows lie together
+  const int h = u % a.c.n_kv_head; u /= a.c.n_kv_head;
+  const int kind = u & 1, i0 = (u >> 1) % a.span, req = (u >> 1) / a.span;
   const int64_t cap = (int64_t)a.c.n_block * BYTE_BLOCK;
   const int len = (int)min((int64_t)max(a.lens[req], 0), cap);
   const int from = a.first ? max(a.first[req], 0) : 0;
@@ -272,6 +310,12 @@ struct ByteAttnArgs {
   float *part;
   int n_row, group, nqg, qt, nsplit, nblk; // group: query heads per key head; nqg: groups of 16 qt (row, query head) columns
   float scale_log2, scale_low;             // log2(e) times the scale, and what its rounding left
+  // CTX: a decode step over a decoder's context.  Rows and queries are the step's (fragments of high and low halves), the first
+  // nblk blocks of the context are codes, everything behind them lies in the decoder's own cache of halves.
+  const f16_t *cq, *cq_lo; bf16_t *cout, *cout_lo;
+  const int4 *qinfo; const uint16_t *gen_sub;
+  const f16_t *hk, *hv;
+  int gen_stride, kv_cap, L, req0;
 };
 
 // Four codes as four halves, exactly: a byte with its sign bit turned is code + 128, under 0x64 it is the half 1024 + 128 +
@@ -332,13 +376,16 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 //    units, which are what binds pieces of a prompt.
 // PP: probabilities as pairs of halves (22 bits): fp32 outputs need them, and half outputs are rounded as finely as single
 // probabilities would be (error of the whole 1.3 times the output's rounding without).
-template <typename T, int HD, bool PP, int QT, int NW>
+// CTX: the columns are a decode step's rows, which see the context up to their limit and generated tokens by their tags.  32 tokens
+// of halves are as many bytes as 64 of codes, and the two kinds of blocks are dealt round-robin as one sequence.
+template <typename T, int HD, bool PP, int QT, int NW, bool CTX = false>
 __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
+  static_assert(!CTX || (QT == 1 && !PP && sizeof(T) == 2), "decode steps: one tile of rows");
   constexpr int NS = HD / 32, NT = HD / 16;              // contraction steps of the scores, 16-dim tiles of the outputs
   constexpr int KW = HD / 64;                            // 16-byte loads per key and lane (8 bytes more where a step is left)
   constexpr int PSTR = HD + 2;
   constexpr int NP = sizeof(T) == 2 && !PP ? 2 : 3, NC = (HD + 63) / 64;     // bytes of a query value; contraction steps of 64
-  constexpr bool QP = sizeof(T) == 4;
+  constexpr bool QP = sizeof(T) == 4 || CTX;
   constexpr float SLACK = slack_of(PP), P_BITS = 15.f - SLACK;
   __shared__ uint4 sm_qi[QT][NP][NC][64], sm_q[QT][(QP ? 2 : 1) * NS][64];
   __shared__ float sm_qf[QT][2][16];
@@ -356,9 +403,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   } else {
     split = u % a.nsplit; unit = u / a.nsplit; qg = 0;
   }
-  const int h = unit % a.c.n_kv_head, req = unit / a.c.n_kv_head;
+  const int h = unit % a.c.n_kv_head, reqi = unit / a.c.n_kv_head, req = CTX ? a.req0 + reqi : reqi;
   const int n_cols = a.n_row * a.group;
-  const size_t rhz = (size_t)unit;
+  const size_t rhz = CTX ? (size_t)req * a.c.n_kv_head + h : (size_t)unit;
+  const int d_model = a.c.n_kv_head * HD;
+  // CTX: the row of column n (clamped: loads stay in bounds) and what it is
+  const int crow = CTX ? reqi * a.n_row + min(qg * 16 + n, a.n_row - 1) : 0;
+  int4 qi = make_int4(0, 0, 0, 0);
+  if constexpr (CTX) qi = a.qinfo[crow];
 
   // One block per wave is in flight while another is worked on: its keys are requested when the scores have taken the ones
   // before, its values when the outputs have.  The first is requested before anything else is read (a wave without one asks for
@@ -414,7 +466,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 #pragma unroll
       for (int j = 0; j < DP; ++j) x[it][j] = 0.f;
       if (qt >= QT) continue;
-      if (col < n_cols) {
+      if (CTX) {
+        if (col < n_cols)
+#pragma unroll
+          for (int j = 0; j < DP; ++j) {
+            const size_t at = act_off(reqi * a.n_row + col, h * HD + pt * DP + j, d_model);
+            x[it][j] = (float)a.cq[at] + (a.cq_lo ? (float)a.cq_lo[at] : 0.f);
+          }
+      } else if (col < n_cols) {
         const int row = col / a.group, hq = h * a.group + col % a.group;
         const T *p = (const T *)a.q + req * a.q_req + row * a.q_row + hq * a.q_head + pt * DP;
 #pragma unroll
@@ -455,8 +514,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
         const int gg = wide ? (d & 63) >> 4 : (d & 31) >> 3, step = wide ? (d >> 6) * 2 + ((d >> 3) & 1) : 2 * KW;
         const float y = x[it][j] * down * sign;
         const f16_t hi = (f16_t)y;
-        ((f16_t *)&sm_q[qt][step][gg * 16 + m])[d & 7] = hi;
-        if (QP) ((f16_t *)&sm_q[qt][(QP ? NS : 0) + step][gg * 16 + m])[d & 7] = (f16_t)(y - (float)hi);
+        // (CTX: the decoder's cache has the dims of a step in their order)
+        const int hs = CTX ? d >> 5 : step, hg = CTX ? (d & 31) >> 3 : gg;
+        ((f16_t *)&sm_q[qt][hs][hg * 16 + m])[d & 7] = hi;
+        if (QP) ((f16_t *)&sm_q[qt][(QP ? NS : 0) + hs][hg * 16 + m])[d & 7] = (f16_t)(y - (float)hi);
         int w = finite ? (int)rintf(x[it][j] * up) : 0;
 #pragma unroll
         for (int b = NP - 1; b >= 0; --b) {
@@ -469,22 +530,34 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   }
   // ---- what the columns see ----
   const int cap = a.c.n_block * BYTE_BLOCK;
-  const int n_keys = min(max(a.lens[req], 0), cap);
+  const int n_keys = CTX ? a.lens[req] : min(max(a.lens[req], 0), cap);
   int lim[QT], tag[QT], reach = 0, lim_all = 0x7fffffff, tag_all = 0x7fffffff;
+  bool qvalid = true;
+  if constexpr (CTX) {
+    qvalid = qg * 16 + n < a.n_row && (qi.x & ROW_VALID);
+    lim[0] = qvalid ? min(qi.z, n_keys) : 0;
+    tag[0] = qvalid ? qi.y : -1;
+    reach = qvalid ? (n_keys > a.L && qi.y >= 1 ? n_keys : lim[0]) : 0;
+    if (qvalid) lim_all = lim[0];
+  } else {
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    const int col = (qg * QT + qt) * 16 + n, row = min(col, n_cols - 1) / a.group;
-    lim[qt] = col < n_cols ? n_keys : 0;
-    if (a.row_limit) lim[qt] = min(lim[qt], max(a.row_limit[(size_t)req * a.n_row + row], 0));
-    tag[qt] = a.key_tag ? a.row_tag[(size_t)req * a.n_row + row] : 0;
-    reach = max(reach, lim[qt]);
-    if (col < n_cols) { lim_all = min(lim_all, lim[qt]); tag_all = min(tag_all, tag[qt]); }
+    for (int qt = 0; qt < QT; ++qt) {
+      const int col = (qg * QT + qt) * 16 + n, row = min(col, n_cols - 1) / a.group;
+      lim[qt] = col < n_cols ? n_keys : 0;
+      if (a.row_limit) lim[qt] = min(lim[qt], max(a.row_limit[(size_t)req * a.n_row + row], 0));
+      tag[qt] = a.key_tag ? a.row_tag[(size_t)req * a.n_row + row] : 0;
+      reach = max(reach, lim[qt]);
+      if (col < n_cols) { lim_all = min(lim_all, lim[qt]); tag_all = min(tag_all, tag[qt]); }
+    }
   }
   reach = __builtin_amdgcn_readfirstlane(fold_row(reach, Max()));
   lim_all = __builtin_amdgcn_readfirstlane(fold_row(lim_all, Min()));
   tag_all = __builtin_amdgcn_readfirstlane(fold_row(tag_all, Min()));
-  const int whole = n_keys / BYTE_BLOCK;                 // blocks of codes; the next one is the tail
-  const int end = min((reach + BYTE_BLOCK - 1) / BYTE_BLOCK, a.nblk), sealed_end = min(end, whole);
+  const int whole = CTX ? a.nblk : n_keys / BYTE_BLOCK;  // blocks of codes; the next one is the tail (CTX: the first of halves)
+  // (CTX: one sequence, 32 tokens of halves a block)
+  const int end = CTX ? (reach <= a.nblk * BYTE_BLOCK ? (reach + BYTE_BLOCK - 1) / BYTE_BLOCK : (reach + 31) / 32 - a.nblk)
+                      : min((reach + BYTE_BLOCK - 1) / BYTE_BLOCK, a.nblk);
+  const int sealed_end = min(end, whole);
   __syncthreads();
   float qf[QT];
 #pragma unroll
@@ -502,6 +575,74 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) ones.hh[e] = (f16_t)1.f;
 
+  // CTX: blocks of 32 tokens of halves; place b of the sequence is block b + nblk of the decoder's cache (clamped: requested
+  // unconditionally)
+  uint4 hk[CTX ? 2 : 1][CTX ? NS : 1], hv[CTX ? NT : 1], htag;
+  const uint4 *HK = (const uint4 *)(a.hk + ((size_t)req * a.c.n_kv_head + h) * a.kv_cap * HD) + lane;
+  const uint4 *HV = (const uint4 *)(a.hv + ((size_t)req * a.c.n_kv_head + h) * a.kv_cap * HD) + lane;
+  const int h_last = a.kv_cap / 32 - 1, L8 = a.L & ~7;
+  auto load_hk = [&](int b) {
+    const size_t hb = min(b + a.nblk, h_last);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < NS; ++c) hk[CTX ? t : 0][CTX ? c : 0] = HK[((hb * 2 + t) * NS + c) * 64];
+    htag = *(const uint4 *)(a.gen_sub + (size_t)req * a.gen_stride + min(max((int)hb * 32 + 8 * g - L8, 0), a.gen_stride - 8));
+  };
+  auto load_hv = [&](int b) {
+    const size_t hb = min(b + a.nblk, h_last);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) hv[CTX ? i : 0] = HV[(hb * NT + i) * 64];
+  };
+  auto half_block = [&]() {
+    floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int c = 0; c < NS; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        Frag f, q;
+        f.u = hk[CTX ? t : 0][CTX ? c : 0];
+        q.u = sm_q[0][c][lane];
+        s[t] = mfma16h(f, q, s[t]);
+        q.u = sm_q[0][(QP ? NS : 0) + c][lane];
+        s[t] = mfma16h(f, q, s[t]);
+      }
+    union { uint4 u; uint16_t t[8]; } tags;
+    tags.u = htag;
+    load_hk(kb + stride);
+    __builtin_amdgcn_sched_barrier(0);
+    if (vref == 0.f) vref = 1.f;
+    const int key0 = (kb + a.nblk) * 32 + 8 * g;          // element e: token key0 + e
+    const float kf = sm_qf[0][1][n];
+    float sv[8], mloc = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int key = key0 + e;
+      const bool vis = (key < lim[0]) | ((key >= a.L) & (key < n_keys) & ((int)tags.t[e] <= tag[0]));
+      sv[e] = vis ? s[e >> 2][e & 3] * kf : -INFINITY;
+      mloc = fmaxf(mloc, sv[e]);
+    }
+    mloc = ceilf(fold32(fold16(mloc, Max()), Max()));
+    const float m_new = mloc > m_run[0] + SLACK ? mloc : m_run[0], m_ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(m_run[0] - m_ref);
+    m_run[0] = m_new;
+    Frag ph;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ph.hh[e] = (f16_t)__builtin_amdgcn_exp2f(sv[e] + (P_BITS - m_ref));
+    const floatx4 t = mfma16h(ones, ph, floatx4{0.f, 0.f, 0.f, 0.f});
+    l_run[0] = fmaf(l_run[0], alpha, t[0]);
+    const float f = 1.f / vref;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      Frag v;
+      v.u = hv[CTX ? i : 0];
+      const floatx4 y = mfma16h(v, ph, floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[0][i][e] = fmaf(y[e], f, o[0][i][e] * alpha);
+    }
+    load_hv(kb + stride);
+    kb += stride;
+  };
   // KIND: 0 a block of codes with another one behind it, 1 the wave's last one, 2 the tail.  (Requests stand outside of all
   // branches: where a branch decides on one, waits count on its not having been made, and where two make it, what arrives is
   // waited for and copied.)
@@ -585,6 +726,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       whole_seen = uniform(whole_seen);
     }
     if (KIND == 0) load_k(kb + stride);
+    if (KIND == 1 && CTX) load_hk(kb + stride);
     __builtin_amdgcn_sched_barrier(0);
     // ---- probabilities ----
     const float vs = TAIL ? 1.f : __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(vsc)));
@@ -688,11 +830,17 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       }
     }
     if (KIND == 0) load_v(kb + stride);
+    if (KIND == 1 && CTX) load_hv(kb + stride);
     kb += stride;
   };
   while (kb + stride < sealed_end) block(std::integral_constant<int, 0>());
   if (kb < sealed_end) block(std::integral_constant<int, 1>());
-  if (kb < end) block(std::integral_constant<int, 2>());          // (end is at most one beyond)
+  else if (CTX) { load_hk(kb); load_hv(kb); }
+  if constexpr (CTX) {
+    while (kb < end) half_block();
+  } else if (kb < end) {
+    block(std::integral_constant<int, 2>());                      // (end is at most one beyond)
+  }
 
   // ---- the waves' states become one ----
 #pragma unroll
@@ -715,7 +863,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     }
     const int col = (qg * QT + qt) * 16 + n;
     if (a.nsplit > 1) {
-      float *pp = a.part + (((size_t)unit * a.nqg + qg) * QT + qt) * a.nsplit * (size_t)(PSTR * 16) + split * (size_t)(PSTR * 16);
+      const size_t pu = CTX ? ((size_t)reqi * a.nqg + qg) * a.c.n_kv_head + h : ((size_t)unit * a.nqg + qg) * QT + qt;
+      float *pp = a.part + pu * a.nsplit * (size_t)(PSTR * 16) + split * (size_t)(PSTR * 16);
       if (wave == 0 && g == 0) { pp[n] = M; pp[16 + n] = L; }
       for (int i = wave; i < NT; i += NW) {
         floatx4 y = fw[0] * sm_o[0][i][lane];
@@ -725,7 +874,18 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       }
       continue;
     }
-    if (col >= n_cols) continue;
+    if (CTX ? !qvalid : col >= n_cols) continue;
+    if constexpr (CTX) {
+      const float inv = 1.f / L;
+      for (int i = wave; i < NT; i += NW) {
+        floatx4 y = fw[0] * sm_o[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) y += fw[w] * sm_o[w][i][lane];
+        const float r[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+        store4_split(a.cout, a.cout_lo, act_off(crow, h * HD + i * 16 + 4 * g, d_model), r);
+      }
+      continue;
+    }
     const size_t at = ((size_t)req * a.n_row + col / a.group) * a.c.n_kv_head * a.group + h * a.group + col % a.group;
     const float inv = L == 0.f ? 0.f : 1.f / L;
     if (a.lse && wave == 0 && g == 0) a.lse[at] = (M + (__builtin_amdgcn_logf(L) - P_BITS)) * 0.6931471805599453f;
@@ -956,4 +1116,151 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
 #undef PD_ATTEND_QT
   PD_CHECK_HIP(hipGetLastError());
   return PD_OK;
+}
+
+// ---------------------------------------------------------------------------
+// a decoder's context
+// ---------------------------------------------------------------------------
+// One work-group per (request, head, block of the context, keys or values): halves of the decoder's cache (two of its blocks of 32
+// tokens), codes of this one.
+template <int HD>
+__global__ __launch_bounds__(256, 3) void k_byte_context(ByteCache c, const f16_t *kc, const f16_t *vc, int kv_cap, int n_whole) {
+  constexpr int P = HD + 8;
+  __shared__ f16_t tile[BYTE_BLOCK * P];
+  __shared__ uint32_t sm_top[4];
+  int u = blockIdx.x;
+  const int h = u % c.n_kv_head; u /= c.n_kv_head;
+  const int kind = u & 1, b = (u >> 1) % n_whole, req = (u >> 1) / n_whole;
+  const size_t rhz = (size_t)req * c.n_kv_head + h;
+  const uint4 *src = (const uint4 *)((kind ? vc : kc) + rhz * kv_cap * HD) + (size_t)b * BYTE_BLOCK * HD / 8;
+  uint32_t top = 0;
+#pragma unroll
+  for (int it = 0; it < HD / 32; ++it) {
+    const int e = threadIdx.x + it * 256, lane = e & 63, m = lane & 15, g = lane >> 4;
+    union { uint4 q; f16_t h[8]; } y;
+    y.q = src[e];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, magnitude(y.h[j]));
+    if (!kind) {                                         // fragment (32 tokens, tile, 32 dims): 8 dims of a token
+      const int c32 = (e >> 6) % (HD / 32), t = (e >> 6) / (HD / 32);
+      *(uint4 *)&tile[((t >> 1) * 32 + 8 * (m >> 2) + 4 * (t & 1) + (m & 3)) * P + c32 * 32 + g * 8] = y.q;
+    } else {                                             // fragment (32 tokens, 16 dims): 8 tokens of a dim
+      const int hb = (e >> 6) % (HD / 16), t32 = (e >> 6) / (HD / 16);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) tile[(t32 * 32 + 8 * g + j) * P + hb * 16 + m] = y.h[j];
+    }
+  }
+  seal_block<HD, P>(tile, sm_top, top, kind, c, rhz * c.n_block + b);
+}
+
+static ByteCache context_cache(const pd_ctx *c, const LayerPtrs &lp) {
+  return ByteCache{lp.b_k, lp.b_v, lp.b_ks, lp.b_vs, nullptr, nullptr, c->B, c->cfg.n_head, c->byte_blocks_cap};
+}
+
+int byte_context_seal(pd_ctx *c, hipStream_t s) {
+  const int n = c->L / BYTE_BLOCK, H = c->cfg.n_head;
+  if (n == 0) return PD_OK;
+  int rc = check_grid((int64_t)c->B * H * n * 2);
+  if (rc) return rc;
+  const dim3 grid((unsigned)(c->B * H * n * 2));
+  for (const LayerPtrs &lp : c->layers) {
+    if (!lp.b_k) continue;
+    const ByteCache bc = context_cache(c, lp);
+    const f16_t *kc = (const f16_t *)lp.kc, *vc = (const f16_t *)lp.vc;
+    switch (c->cfg.head_dim) {
+      case 32: hipLaunchKernelGGL(k_byte_context<32>, grid, dim3(256), 0, s, bc, kc, vc, c->kv_cap, n); break;
+      case 64: hipLaunchKernelGGL(k_byte_context<64>, grid, dim3(256), 0, s, bc, kc, vc, c->kv_cap, n); break;
+      case 96: hipLaunchKernelGGL(k_byte_context<96>, grid, dim3(256), 0, s, bc, kc, vc, c->kv_cap, n); break;
+      default: hipLaunchKernelGGL(k_byte_context<128>, grid, dim3(256), 0, s, bc, kc, vc, c->kv_cap, n); break;
+    }
+  }
+  PD_CHECK_HIP(hipGetLastError());
+  return PD_OK;
+}
+
+int byte_context_attention(pd_ctx *c, const LayerPtrs &lw, int A, int nreq, int req0, hipStream_t s, int *splits) {
+  const pd_config &g = c->cfg;
+  ByteAttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.c = context_cache(c, lw);
+  a.c.n_req = nreq;
+  a.cq = (const f16_t *)c->q; a.cq_lo = (const f16_t *)mfma_lo(c, c->q, g.d_model);
+  a.cout = (bf16_t *)c->att; a.cout_lo = mfma_lo(c, c->att, g.d_model);
+  a.qinfo = c->rows.qinfo; a.gen_sub = c->sch.gen_sub; a.lens = c->sch.kv_len;
+  a.hk = (const f16_t *)lw.kc; a.hv = (const f16_t *)lw.vc;
+  a.gen_stride = c->gen_stride; a.kv_cap = c->kv_cap; a.L = c->L; a.req0 = req0;
+  a.n_row = A; a.group = 1; a.nqg = (A + 15) / 16; a.qt = 1; a.nblk = c->L / BYTE_BLOCK;
+  a.part = c->att_part;
+  const double scale = 1.4426950408889634 / std::sqrt((double)g.head_dim);
+  a.scale_log2 = (float)scale;
+  // blocks of the middle of the run; the tokens behind the whole blocks are halves, 32 a block
+  const int tail = c->L % BYTE_BLOCK + c->S * (c->M + 1) / 2;
+  const int64_t units = (int64_t)nreq * a.nqg * g.n_head;
+  PD_REQUIRE(units <= c->part_units, PD_EINVAL, "too many (request, head, query group) units: %lld", (long long)units);
+  const ByteAttnShape shape = byte_attn_shape(16, units, a.nblk + (tail + 31) / 32);
+  a.nsplit = c->opt_splits > 0 ? c->opt_splits : shape.splits;
+  a.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(a.nsplit, c->part_units / units));
+  *splits = a.nsplit;
+  const int64_t grid = (a.nqg > 1 ? ((int64_t)nreq * g.n_head + 7) / 8 * 8 * a.nqg : units) * a.nsplit;
+  int rc = check_grid(grid);
+  if (rc) return rc;
+#define PD_CONTEXT(HDV)                                                                                                       \
+  do {                                                                                                                        \
+    if (shape.waves == 8)                                                                                                     \
+      hipLaunchKernelGGL((k_byte_attn<bf16_t, HDV, false, 1, 8, true>), dim3((unsigned)grid), dim3(512), 0, s, a);            \
+    else                                                                                                                      \
+      hipLaunchKernelGGL((k_byte_attn<bf16_t, HDV, false, 1, 4, true>), dim3((unsigned)grid), dim3(256), 0, s, a);            \
+  } while (0)
+  switch (g.head_dim) {
+    case 32: PD_CONTEXT(32); break;
+    case 64: PD_CONTEXT(64); break;
+    case 96: PD_CONTEXT(96); break;
+    default: PD_CONTEXT(128); break;
+  }
+#undef PD_CONTEXT
+  PD_CHECK_HIP(hipGetLastError());
+  return PD_OK;
+}
+
+static size_t context_layer_bytes(const pd_ctx *c) {
+  const size_t units = (size_t)c->cfg.max_batch * c->cfg.n_head, blocks = (size_t)c->cfg.max_ctx / BYTE_BLOCK;
+  const size_t codes = units * blocks * BYTE_BLOCK * c->cfg.head_dim, scales = (units * blocks * sizeof(float) + 255) / 256 * 256;
+  return 2 * ((codes + 255) / 256 * 256 + scales);
+}
+static int context_layers(const pd_ctx *c) {
+  int n = 0;
+  for (const LayerPtrs &lp : c->layers) n += lp.kc_lo ? 0 : 1;
+  return n;
+}
+
+extern "C" size_t pd_byte_context_bytes(const pd_ctx *c) {
+  if (!c || c->arch == 1 || c->impl != 1) return 0;
+  return std::max<size_t>(256, context_layers(c) * context_layer_bytes(c));
+}
+
+extern "C" int pd_byte_context(pd_ctx *c, void *dev_buffer, size_t bytes, void *hip_stream) {
+  PD_REQUIRE(c, PD_EINVAL, "ctx is NULL");
+  if (dev_buffer) {
+    PD_REQUIRE(c->arch == 0 && c->impl == 1, PD_EINVAL,
+               "an 8-bit context needs a decoder-only configuration on the matrix-core kernels");
+    PD_REQUIRE(((uintptr_t)dev_buffer & 255) == 0, PD_EINVAL, "the buffer must be 256-byte aligned");
+    const size_t need = pd_byte_context_bytes(c);
+    PD_REQUIRE(bytes >= need, PD_ENOMEM, "buffer too small: %zu bytes given, %zu needed", bytes, need);
+  }
+  byte_context_drop_graph(c);
+  const size_t units = (size_t)c->cfg.max_batch * c->cfg.n_head, blocks = (size_t)c->cfg.max_ctx / BYTE_BLOCK;
+  const size_t codes = (units * blocks * BYTE_BLOCK * c->cfg.head_dim + 255) / 256 * 256;
+  const size_t scales = (units * blocks * sizeof(float) + 255) / 256 * 256;
+  c->byte_blocks_cap = (int)blocks;
+  c->byte_context = dev_buffer != nullptr;
+  char *p = (char *)dev_buffer;
+  for (LayerPtrs &lp : c->layers) {
+    const bool on = dev_buffer && !lp.kc_lo && blocks;
+    lp.b_k = on ? (int8_t *)p : nullptr;
+    lp.b_v = on ? (int8_t *)(p + codes) : nullptr;
+    lp.b_ks = on ? (float *)(p + 2 * codes) : nullptr;
+    lp.b_vs = on ? (float *)(p + 2 * codes + scales) : nullptr;
+    if (on) p += 2 * (codes + scales);
+  }
+  return c->byte_context && c->prefilled ? byte_context_seal(c, (hipStream_t)hip_stream) : PD_OK;
 }

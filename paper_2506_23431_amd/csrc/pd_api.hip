@@ -259,6 +259,7 @@ __global__ void k_fill_zero(uint4 *p, size_t n16) {
 // the workspace, re-packing the weights.  `c` has its configuration, pointers and carve-up.
 static int finish_create(pd_ctx *c, size_t need, void *hip_stream, bool no_alloc, pd_ctx **out) {
   c->prefilled = false; c->host_steps = 0;
+  c->byte_context = false; c->byte_blocks_cap = 0;
   c->embed_pending = false; c->embedded = false; c->norm_fused = c->norm_halves = false; c->packed = false;
   c->opt_splits = 0; c->opt_graph = 0; c->opt_profile = 0; c->opt_split = 1; c->opt_chunk = 0; c->opt_fuse_norm = 1;
   c->opt_ctx_split = 1; c->opt_ctx_attn = 1;
@@ -488,6 +489,8 @@ static void drop_graph(pd_ctx *c) {
   c->graph_exec = nullptr; c->graph_ready = false;
 }
 
+void byte_context_drop_graph(pd_ctx *c) { drop_graph(c); }
+
 extern "C" int pd_set_option(pd_ctx *c, int key, int value) {
   PD_REQUIRE(c, PD_EINVAL, "ctx is NULL");
   switch (key) {
@@ -541,6 +544,7 @@ extern "C" int pd_get_info(pd_ctx *c, int key, void *hip_stream, int64_t *value)
     case PD_INFO_KV_PAIR_LAYERS: *value = c->pair_layers; return PD_OK;
     case PD_INFO_CONTEXT_PAIRS: *value = context_pairs(c) ? 1 : 0; return PD_OK;
     case PD_INFO_STREAM_LOADS: *value = c->stream_loads; return PD_OK;
+    case PD_INFO_BYTE_BLOCKS: *value = c->byte_context && c->prefilled ? c->L / PD_BYTE_BLOCK : 0; return PD_OK;
     case PD_INFO_KEPT_BYTES: *value = mfma_kept_bytes(c); return PD_OK;
     case PD_INFO_KV_SATURATED: {
       hipStream_t s = (hipStream_t)hip_stream;
@@ -649,6 +653,7 @@ extern "C" int pd_prefill_context(pd_ctx *c, const int32_t *ctx_tokens, int B, i
     b += nreq;
   }
   c->opt_split = split_decode;
+  if (!rc && c->byte_context) rc = byte_context_seal(c, s);
   if (rc) return rc;
   // leave the row tables empty so that a stray head/commit sees no rows
   if ((rc = launch_reset_state(c, s))) return rc;

@@ -170,6 +170,7 @@ struct LayerPtrs {
   const float *n3g;                                // gain of the norm in front of it
   bf16_t *p_cq, *p_ckv, *p_co;
   void *xkc, *xvc;                                 // keys / values of the encoder states, this layer's projection
+  int8_t *b_k, *b_v; float *b_ks, *b_vs;           // the context's whole blocks in 8 bits (pd_byte_context), else NULL
 };
 
 // What pd_encdec_create adds to a context (Eq. 1 as the paper runs it: a stacked encoder, a decoder with
@@ -251,6 +252,8 @@ struct pd_ctx : RowSet {    // (the set in use: decode steps, passes over one re
   double *loss;             // [B]
   int32_t *tf_target;       // [B][S][M + 2] device copy of the training targets
   bool prefilled;
+  bool byte_context;        // decode steps read the context's whole blocks of 64 tokens from 8-bit codes (layers without pairs)
+  int byte_blocks_cap;      // such blocks that the codes have room for per request and head
   int host_steps;           // decode steps enqueued since prefill/reset
   // options
   int opt_splits, opt_graph, opt_profile, opt_split, opt_chunk, opt_fuse_norm, opt_ctx_split, opt_ctx_attn;
@@ -288,6 +291,10 @@ int mfma_layer(pd_ctx *c, int l, int R, int A, int nreq, int req0, int kv_overri
 // logits != NULL: the logits of the rows that carry a token go there; tf_A == 0: [B][S][vocab], at the place of the
 // row's request and subsequence; tf_A > 0 (teacher-forced pass, tf_A rows per request): [requests][tf_cap][vocab]
 int mfma_head(pd_ctx *c, int R, float *logits, hipStream_t s, int tf_A = 0, int tf_cap = 0);
+// 8-bit context (byte_cache.hip)
+int byte_context_seal(pd_ctx *c, hipStream_t s);      // codes of the encoded contexts
+int byte_context_attention(pd_ctx *c, const LayerPtrs &lw, int A, int nreq, int req0, hipStream_t s, int *splits);
+void byte_context_drop_graph(pd_ctx *c);               // (pd_api.hip)
 // encoder-decoder form (encdec.hip)
 int encdec_pack_weights(pd_ctx *c, hipStream_t s);
 int encdec_build_tables(pd_ctx *c, int *scratch, hipStream_t s);
