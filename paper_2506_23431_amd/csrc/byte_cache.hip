@@ -387,7 +387,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   constexpr int NP = sizeof(T) == 2 && !PP ? 2 : 3, NC = (HD + 63) / 64;     // bytes of a query value; contraction steps of 64
   constexpr bool QP = sizeof(T) == 4 || CTX;
   constexpr float SLACK = slack_of(PP), P_BITS = 15.f - SLACK;
-  __shared__ uint4 sm_qi[QT][NP][NC][64], sm_q[QT][(QP ? 2 : 1) * NS][64];
+  __shared__ uint4 sm_qi[QT][NP][NC][64], sm_q[CTX ? 1 : QT][CTX ? 1 : (QP ? 2 : 1) * NS][64];
   __shared__ float sm_qf[QT][2][16];
   __shared__ uint32_t sm_top[QT][16][16];
   __shared__ float sm_m[QT][NW][16], sm_l[QT][NW][16];
@@ -451,34 +451,55 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) vw[i] = ld_code<QT == 1, uint4>(vp + i * 256);
   };
+  // ---- the queries of the columns: dims and columns dealt over all threads (columns beyond the last: that one's) ----
+  // They are asked for first, so that they are not waited for behind the keys and values of the first block.
+  constexpr int DP = HD / 16;                            // dims per (column, part)
+  constexpr int IT = (QT * 256 + NW * 64 - 1) / (NW * 64);
+  T xq[CTX ? 1 : IT][DP];
+  f16_t xh[CTX ? IT : 1][2][DP];                         // CTX: high and low halves
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int e = threadIdx.x + it * NW * 64, qt = e >> 8, pt = e >> 4 & 15;
+    const int col = min((qg * QT + min(qt, QT - 1)) * 16 + (e & 15), n_cols - 1);
+    if constexpr (CTX) {
+      const size_t at = act_off(reqi * a.n_row + col, h * HD + pt * DP, d_model);
+      const f16_t *lo = a.cq_lo ? a.cq_lo : a.cq;
+      if constexpr (HD != 96) {                          // (they lie in one granule of 8)
+        typedef f16_t part_t __attribute__((ext_vector_type(DP)));
+        union { part_t v; f16_t h[DP]; } u[2];
+        u[0].v = *(const part_t *)(a.cq + at);
+        u[1].v = *(const part_t *)(lo + at);
+#pragma unroll
+        for (int j = 0; j < DP; ++j) { xh[it][0][j] = u[0].h[j]; xh[it][1][j] = u[1].h[j]; }
+      } else {
+#pragma unroll
+        for (int j = 0; j < DP; ++j) {
+          const size_t one = act_off(reqi * a.n_row + col, h * HD + pt * DP + j, d_model);
+          xh[it][0][j] = a.cq[one]; xh[it][1][j] = lo[one];
+        }
+      }
+    } else {
+      const int row = a.group == 1 ? col : col / a.group;
+      const T *p = (const T *)a.q + req * a.q_req + row * a.q_row + (h * a.group + col - row * a.group) * a.q_head + pt * DP;
+#pragma unroll
+      for (int j = 0; j < DP; ++j) xq[CTX ? 0 : it][j] = p[j];
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
   load_k(min(kb, a.c.n_block - 1));
   load_v(min(kb, a.c.n_block - 1));
   __builtin_amdgcn_sched_barrier(0);
 
-  // ---- the queries of the columns, in operand order: whole numbers of NP bytes for the codes, halves for the tail ----
+  // ... in operand order: whole numbers of NP bytes for the codes, halves for the tail
   {
-    constexpr int DP = HD / 16;                          // dims per (column, part)
-    constexpr int IT = (QT * 256 + NW * 64 - 1) / (NW * 64);
     float x[IT][DP];
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
-      const int e = threadIdx.x + it * NW * 64, qt = e >> 8, pt = e >> 4 & 15, col = (qg * QT + qt) * 16 + (e & 15);
+      const int e = threadIdx.x + it * NW * 64, qt = e >> 8, pt = e >> 4 & 15;
 #pragma unroll
-      for (int j = 0; j < DP; ++j) x[it][j] = 0.f;
+      for (int j = 0; j < DP; ++j)
+        x[it][j] = CTX ? (float)xh[CTX ? it : 0][0][j] + (a.cq_lo ? (float)xh[CTX ? it : 0][1][j] : 0.f) : ld_f32(&xq[CTX ? 0 : it][j], 0);
       if (qt >= QT) continue;
-      if (CTX) {
-        if (col < n_cols)
-#pragma unroll
-          for (int j = 0; j < DP; ++j) {
-            const size_t at = act_off(reqi * a.n_row + col, h * HD + pt * DP + j, d_model);
-            x[it][j] = (float)a.cq[at] + (a.cq_lo ? (float)a.cq_lo[at] : 0.f);
-          }
-      } else if (col < n_cols) {
-        const int row = col / a.group, hq = h * a.group + col % a.group;
-        const T *p = (const T *)a.q + req * a.q_req + row * a.q_row + hq * a.q_head + pt * DP;
-#pragma unroll
-        for (int j = 0; j < DP; ++j) x[it][j] = ld_f32(p, j);
-      }
       uint32_t top = 0;
 #pragma unroll
       for (int j = 0; j < DP; ++j) top = max(top, __float_as_uint(x[it][j]) & 0x7fffffffu);
@@ -512,12 +533,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
         // dim -> (step of 64, group, byte) for the codes; 16 dims of a 16-byte load are 8 of two steps of 32 for the halves
         const bool wide = d < KW * 64;
         const int gg = wide ? (d & 63) >> 4 : (d & 31) >> 3, step = wide ? (d >> 6) * 2 + ((d >> 3) & 1) : 2 * KW;
-        const float y = x[it][j] * down * sign;
-        const f16_t hi = (f16_t)y;
-        // (CTX: the decoder's cache has the dims of a step in their order)
-        const int hs = CTX ? d >> 5 : step, hg = CTX ? (d & 31) >> 3 : gg;
-        ((f16_t *)&sm_q[qt][hs][hg * 16 + m])[d & 7] = hi;
-        if (QP) ((f16_t *)&sm_q[qt][(QP ? NS : 0) + hs][hg * 16 + m])[d & 7] = (f16_t)(y - (float)hi);
+        if constexpr (!CTX) {
+          const float y = x[it][j] * down * sign;
+          const f16_t hi = (f16_t)y;
+          ((f16_t *)&sm_q[qt][step][gg * 16 + m])[d & 7] = hi;
+          if (QP) ((f16_t *)&sm_q[qt][(QP ? NS : 0) + step][gg * 16 + m])[d & 7] = (f16_t)(y - (float)hi);
+        }
         int w = finite ? (int)rintf(x[it][j] * up) : 0;
 #pragma unroll
         for (int b = NP - 1; b >= 0; --b) {
@@ -578,6 +599,15 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   // CTX: blocks of 32 tokens of halves; place b of the sequence is block b + nblk of the decoder's cache (clamped: requested
   // unconditionally)
   uint4 hk[CTX ? 2 : 1][CTX ? NS : 1], hv[CTX ? NT : 1], htag;
+  Frag hq[CTX ? 2 : 1][CTX ? NS : 1];                    // the step's queries as they are, high and low halves
+  auto load_hq = [&]() {
+    const size_t at = act_off(crow, h * HD + g * 8, d_model);
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+      hq[0][CTX ? c : 0].u = *(const uint4 *)(a.cq + at + (size_t)c * 512);
+      hq[CTX ? 1 : 0][CTX ? c : 0].u = *(const uint4 *)((a.cq_lo ? a.cq_lo : a.cq) + at + (size_t)c * 512);
+    }
+  };
   const uint4 *HK = (const uint4 *)(a.hk + ((size_t)req * a.c.n_kv_head + h) * a.kv_cap * HD) + lane;
   const uint4 *HV = (const uint4 *)(a.hv + ((size_t)req * a.c.n_kv_head + h) * a.kv_cap * HD) + lane;
   const int h_last = a.kv_cap / 32 - 1, L8 = a.L & ~7;
@@ -600,12 +630,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     for (int c = 0; c < NS; ++c)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        Frag f, q;
+        Frag f;
         f.u = hk[CTX ? t : 0][CTX ? c : 0];
-        q.u = sm_q[0][c][lane];
-        s[t] = mfma16h(f, q, s[t]);
-        q.u = sm_q[0][(QP ? NS : 0) + c][lane];
-        s[t] = mfma16h(f, q, s[t]);
+        s[t] = mfma16h(f, hq[0][CTX ? c : 0], s[t]);
+        if (a.cq_lo) s[t] = mfma16h(f, hq[CTX ? 1 : 0][CTX ? c : 0], s[t]);
       }
     union { uint4 u; uint16_t t[8]; } tags;
     tags.u = htag;
@@ -613,7 +641,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     if (vref == 0.f) vref = 1.f;
     const int key0 = (kb + a.nblk) * 32 + 8 * g;          // element e: token key0 + e
-    const float kf = sm_qf[0][1][n];
+    const float kf = a.scale_log2;
     float sv[8], mloc = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -653,14 +681,26 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     const f16_t *vt = (const f16_t *)a.c.v_tail + (rhz * 2 + (kb & 1)) * BYTE_BLOCK * HD + (g * HD + n) * 8;
     const int key0 = kb * BYTE_BLOCK + 4 * g;            // element e: token key0 + 16 (e >> 2) + (e & 3)
     auto key = [&](int e) { return key0 + 16 * (e >> 2) + (e & 3); };
-    Frag vtail[TAIL ? NT : 1][2];
-    if (TAIL)
+    // the tail: everything that its scores need is requested before what its outputs need
+    Frag vtail[TAIL ? NT : 1][2], ktail[TAIL && QT == 1 ? 4 : 1][TAIL && QT == 1 ? NS : 1];
+    auto tail_k = [&](int c, int t) {
+      return *(const uint4 *)(kt + ((c < 2 * KW ? (c >> 1) * 8 + g * 2 + (c & 1) : KW * 8 + g) * BYTE_BLOCK + 16 * t) * 8);
+    };
+    if (TAIL) {
+      if (QT == 1)
+#pragma unroll
+        for (int c = 0; c < NS; ++c)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) ktail[QT == 1 && TAIL ? t : 0][QT == 1 && TAIL ? c : 0].u = tail_k(c, t);
+      load_tags(kb);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         vtail[TAIL ? i : 0][0].u = *(const uint4 *)(vt + i * 128);
         vtail[TAIL ? i : 0][1].u = *(const uint4 *)(vt + 4 * HD * 8 + i * 128);
       }
-    if (TAIL) load_tags(kb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     union { uint2 u[4]; uint16_t s[16]; uint32_t w[8]; } tags;
 #pragma unroll
     for (int t = 0; t < 4; ++t) tags.u[t] = tg[t];
@@ -678,12 +718,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           Frag f, q;
-          f.u = *(const uint4 *)(kt + ((c < 2 * KW ? (c >> 1) * 8 + g * 2 + (c & 1) : KW * 8 + g) * BYTE_BLOCK + 16 * t) * 8);
+          if (QT == 1) f = ktail[QT == 1 && TAIL ? t : 0][QT == 1 && TAIL ? c : 0];
+          else f.u = tail_k(c, t);
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) {
-            q.u = sm_q[qt][c][lane];
+            q.u = sm_q[CTX ? 0 : qt][CTX ? 0 : c][lane];
             s[qt][t] = mfma16h(f, q, s[qt][t]);
-            if (QP) { q.u = sm_q[qt][(QP ? NS : 0) + c][lane]; s[qt][t] = mfma16h(f, q, s[qt][t]); }
+            if (QP) { q.u = sm_q[CTX ? 0 : qt][CTX ? 0 : (QP ? NS : 0) + c][lane]; s[qt][t] = mfma16h(f, q, s[qt][t]); }
           }
         }
 #pragma unroll
@@ -726,7 +767,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       whole_seen = uniform(whole_seen);
     }
     if (KIND == 0) load_k(kb + stride);
-    if (KIND == 1 && CTX) load_hk(kb + stride);
+    if (KIND == 1 && CTX) { load_hq(); load_hk(kb + stride); }
     __builtin_amdgcn_sched_barrier(0);
     // ---- probabilities ----
     const float vs = TAIL ? 1.f : __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(vsc)));
@@ -835,7 +876,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   };
   while (kb + stride < sealed_end) block(std::integral_constant<int, 0>());
   if (kb < sealed_end) block(std::integral_constant<int, 1>());
-  else if (CTX) { load_hk(kb); load_hv(kb); }
+  else if (CTX) { load_hq(); load_hk(kb); load_hv(kb); }
   if constexpr (CTX) {
     while (kb < end) half_block();
   } else if (kb < end) {
