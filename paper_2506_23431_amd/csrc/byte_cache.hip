@@ -1100,7 +1100,7 @@ static int byte_shape(const pd_byte_cache *c, int n_head, int n_row, int max_len
   const int64_t most = max_len ? std::min<int64_t>(max_len, cap) : cap;
   const int64_t heads = (int64_t)c->n_req * c->n_kv_head;
   out->nblk = (int)((most + BYTE_BLOCK - 1) / BYTE_BLOCK);
-  const ByteAttnShape sh = byte_attn_shape(n_row * (n_head / c->n_kv_head), heads, out->nblk);
+  const ByteAttnShape sh = byte_attn_shape(n_row * (n_head / c->n_kv_head), heads, out->nblk, c->head_dim);
   out->qt = sh.tiles; out->waves = sh.waves; out->nsplit = sh.splits;
   out->nqg = sh.groups;
   out->units = heads * sh.groups;
@@ -1238,7 +1238,7 @@ int byte_context_attention(pd_ctx *c, const LayerPtrs &lw, int A, int nreq, int 
   const int tail = c->L % BYTE_BLOCK + c->S * (c->M + 1) / 2;
   const int64_t units = (int64_t)nreq * a.nqg * g.n_head;
   PD_REQUIRE(units <= c->part_units, PD_EINVAL, "too many (request, head, query group) units: %lld", (long long)units);
-  const ByteAttnShape shape = byte_attn_shape(16, units, a.nblk + (tail + 31) / 32);
+  const ByteAttnShape shape = byte_attn_shape(16, units, a.nblk + (tail + 31) / 32, g.head_dim);
   a.nsplit = c->opt_splits > 0 ? c->opt_splits : shape.splits;
   a.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(a.nsplit, c->part_units / units));
   *splits = a.nsplit;

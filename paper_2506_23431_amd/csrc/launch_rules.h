@@ -359,18 +359,20 @@ struct ByteAttnShape { int tiles, groups, splits, waves; };
 
 // cols: query vectors per key head; heads: requests x key heads; nblk: blocks of 64 tokens.
 // Two tiles share the conversion of the values (16 heads, 2048 rows, 6144 tokens of size 128 268 us with one, 155 with two).
-// Eight waves, a work-group per compute unit, with the tokens split over as many of them as there are compute units once a wave
-// would have more than two or three blocks: the second launch that joins the splits costs what 2 blocks of a wave do (us, no
-// split / best split: 12 units of head size 128, 16 blocks 10.2 / 9.9, 32 blocks 15 / 11; 32 units, 63 blocks 24.5 / 13.6, 256 blocks 78 /
-// 26).  Four waves where there is no more than a block for each (12 units, 2 blocks 7.4 against 7.6), and where more units than
-// compute units keep the chip busy with less left over at each end (1024 units, 5 / 16 / 32 blocks 26 / 47 / 87 against 38 / 54 /
-// 95; 63 blocks 161 against 159).
-inline ByteAttnShape byte_attn_shape(int cols, int64_t heads, int nblk) {
+// Eight waves, and the tokens split over as many work-groups as there are compute units where that saves a wave enough blocks: a
+// block costs 0.0175 us per dim (one unit, 16 / 63 blocks without splits: size 128 8.4 / 21.5 us, 64 6.8 / 15.1), the launch that
+// joins the splits 3.5 us (no split / best split: 12 units of size 128, 16 blocks 10.2 / 9.4, 63 blocks 23.4 / 11.3; 32 units, 63 blocks
+// 24.5 / 13.6, 256 blocks 78 / 26; 4 units of size 64, 16 blocks 7.4 / 7.6).  Four waves where there is no more than a block for each
+// (12 units, 2 blocks 7.4 against 7.6), and where more units than compute units keep the chip busy with less left over at each
+// end (1024 units, 5 / 16 / 32 blocks 26 / 47 / 87 against 38 / 54 / 95; 63 blocks 161 against 159).
+inline ByteAttnShape byte_attn_shape(int cols, int64_t heads, int nblk, int head_dim) {
   ByteAttnShape s{cols > 16 ? 2 : 1, 0, 1, 8};
   s.groups = (cols + 16 * s.tiles - 1) / (16 * s.tiles);
   const int64_t units = heads * s.groups;
   if (units < 1) return s;
-  if (nblk > 20) s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / units, nblk / 8));
+  const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / units, nblk / 8));
+  const int saved = (nblk + 7) / 8 - (nblk + 8 * splits - 1) / (8 * splits);
+  if (saved * 0.0175 * head_dim * s.tiles > 3.5) s.splits = splits;
   if (nblk <= 4 || (units > 256 && (nblk < 64 || s.tiles > 1))) s.waves = 4;
   return s;
 }
