@@ -424,7 +424,10 @@ int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const
  * them (the rest of the context and all generated tokens) from the 16-bit cache, which the context pass and pd_teacher_forced
  * go on using for all of it: half of the bytes of the attention's hot loop for a further buffer.  Layers that keep pairs of halves
  * (kv_pair_layers) stay as they are.  A caller's trade, not the library's: keys and values of the context are off by up to half
- * a scale, 1/254 of their block's largest (measured beside the other switches in PD_OPT_CONTEXT_SPLIT_ACT's terms: BYTE_FIGURES).
+ * a scale, 1/254 of their block's largest.  Measured against the same steps over the 16-bit cache, random tokens: 6 layers of width
+ * 768, 12 of 1024, 24 of 2048 move the logits by up to 7.6e-3, 8.8e-3, 1.8e-2 (rms 1.3e-3, 1.5e-3, 2.8e-3 of logits whose own is
+ * 0.56, 0.64, 0.90).  Attention with its merge, us per layer, halves / codes: 12 heads of 64, 1 x 1024 tokens 9.8 / 11.1 (short
+ * contexts lose), 16 heads of 64, 8 x 2048 tokens 18.2 / 15.7, 16 of 128, 1 x 8192 19.5 / 17.8, 32 of 128, 4 x 4096 70 / 58.
  *   dev_buffer  DEVICE, 256-byte aligned, at least pd_byte_context_bytes(ctx) (0: this context cannot have one), to outlive the
  *               ctx or the next such call; NULL: back to the 16-bit cache
  * Contexts that are encoded already get their codes at once, others at the end of pd_prefill_context; asynchronous on

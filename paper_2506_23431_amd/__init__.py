@@ -7,4 +7,10 @@ not been built (there is no CPU fallback).
 """
 
 from .binding import PipelinedDecoder, load, PdError  # noqa: F401
-from .byte_cache import ByteCache  # noqa: F401
+
+
+def __getattr__(name):
+    if name == "ByteCache":             # (imports torch, which the rest does where it is needed)
+        from .byte_cache import ByteCache
+        return ByteCache
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -297,14 +297,14 @@ class PipelinedDecoder:
         """pd_byte_context: decode steps read the whole blocks of 64 tokens of the contexts from 8-bit codes (a buffer of this
         object's holds them); False: back to the 16-bit cache."""
         buffer, base, nbytes = None, None, 0
+        if getattr(self, "_byte_buffer", None) is not None:
+            self.torch.cuda.synchronize(self.device)          # (steps under way, on any stream, may still read the old codes)
         if on:
             nbytes = self.lib.pd_byte_context_bytes(self.ctx)
             if nbytes == 0:
                 raise PdError("an 8-bit context needs a decoder-only configuration on the matrix-core kernels")
             buffer = self.torch.empty(nbytes + 256, dtype=self.torch.uint8, device=self.device)
             base = C.c_void_p((buffer.data_ptr() + 255) // 256 * 256)
-        else:
-            self.torch.cuda.synchronize(self.device)          # (steps under way may still read the codes)
         _check(self.lib.pd_byte_context(self.ctx, base, nbytes, self._stream()))
         self._byte_buffer = buffer
 

@@ -27,7 +27,8 @@ class ByteCache:
 
     How many tokens a request holds is the caller's to know and is passed to every call as `lens`, an int32 tensor [n_req] on the
     cache's device that is read when the kernels run.  Work is queued on the current stream of that device; nothing is kept
-    between calls but the tensors k, v, k_scale, v_scale, k_tail, v_tail, and calls can be captured into a graph."""
+    between calls but the tensors k, v, k_scale, v_scale, k_tail, v_tail, and calls can be captured into a graph.  For inference:
+    no gradients are recorded."""
 
     def __init__(self, n_req, n_kv_head, head_dim, max_tokens, device="cuda:0"):
         device, n_block = torch.device(device), -(-max_tokens // BLOCK)
@@ -48,6 +49,8 @@ class ByteCache:
         self._c = PdByteCache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
                               self.k_tail.data_ptr(), self.v_tail.data_ptr(), n_req, n_kv_head, head_dim, n_block)
         self._p = C.byref(self._c)
+        # (what the pointers lead to lives as long as they do, whatever becomes of the attributes)
+        self._held = (self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail)
 
     # -- in and out, in the plain order of tokens and dims -------------------------
     def to_tensors(self):

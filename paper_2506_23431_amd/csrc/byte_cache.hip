@@ -1303,5 +1303,11 @@ extern "C" int pd_byte_context(pd_ctx *c, void *dev_buffer, size_t bytes, void *
     lp.b_vs = on ? (float *)(p + 2 * codes + scales) : nullptr;
     if (on) p += 2 * (codes + scales);
   }
-  return c->byte_context && c->prefilled ? byte_context_seal(c, (hipStream_t)hip_stream) : PD_OK;
+  if (!c->byte_context || !c->prefilled) return PD_OK;
+  const int rc = byte_context_seal(c, (hipStream_t)hip_stream);
+  if (rc) {                                              // without its codes the context stays in 16 bits
+    c->byte_context = false;
+    for (LayerPtrs &lp : c->layers) lp.b_k = lp.b_v = nullptr;
+  }
+  return rc;
 }

@@ -161,6 +161,32 @@ def test_replayed_steps_and_splits_and_events():
     dec.close()
 
 
+def test_switched_on_again_while_steps_are_under_way():
+    """Another buffer takes the codes; the steps that read the first one, on a stream of their own, keep it until they are done."""
+    import torch
+    cfg = CASES[4]
+    w, ctx = pi.make_weights(cfg, threads=4), pi.make_context(cfg)
+    args = (ctx, cfg.n_sub, cfg.delta_t, cfg.sub_tokens, cfg.time_steps)
+    dec = make_decoder(cfg, w)
+    dec.use_byte_context()
+    dec.prefill_context(*args)
+    dec.decode_steps(cfg.time_steps - 1)
+    want = dec.decode_step(want_logits=True)[1].cpu().numpy()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            dec.reset_decode()
+            dec.decode_steps(cfg.time_steps - 1)
+        dec.use_byte_context()
+        torch.full((dec.lib.pd_byte_context_bytes(dec.ctx),), 77, dtype=torch.uint8, device="cuda:0")   # (takes the freed memory)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            got = dec.decode_step(want_logits=True)[1].cpu().numpy()
+        assert np.array_equal(want, got, equal_nan=True)
+    dec.close()
+
+
 def test_teacher_forced_pass_does_not_see_the_codes():
     cfg = CASES[0]
     w, ctx = pi.make_weights(cfg, threads=4), pi.make_context(cfg)
