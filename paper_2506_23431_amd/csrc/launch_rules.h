@@ -358,7 +358,8 @@ inline RowTiling row_tiling(int n_tiles, int KT, int rows, int max_slices, bool 
 struct ByteAttnShape { int tiles, groups, splits, waves; };
 
 // cols: query vectors per key head; heads: requests x key heads; nblk: blocks of 64 tokens.
-// Two tiles share the conversion of the values (16 heads, 2048 rows, 6144 tokens of size 128 268 us with one, 155 with two).
+// Two tiles share the conversion of the values (us with one / with two: 16 heads, 2048 rows, 6144 tokens of size 128 158 / 118, 8 heads
+// and requests, 999 columns, 1500 tokens of 64 17.4 / 14.7).
 // Eight waves, and the tokens split over as many work-groups as there are compute units where that saves a wave enough blocks: a
 // block costs 0.0175 us per dim (one unit, 16 / 63 blocks without splits: size 128 8.4 / 21.5 us, 64 6.8 / 15.1), the launch that
 // joins the splits 3.5 us (no split / best split: 12 units of size 128, 16 blocks 10.2 / 9.4, 63 blocks 23.4 / 11.3; 32 units, 63 blocks
