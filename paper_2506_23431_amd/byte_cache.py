@@ -44,6 +44,7 @@ class ByteCache:
         self.v_tail = zeros(2, 2, 4, head_dim, 8, dtype=torch.float16)
         self.n_req, self.n_kv_head, self.n_block, self.head_dim = n_req, n_kv_head, n_block, head_dim
         self.device = self.k.device
+        self._index = self.device.index
         self._scale = 1.0 / math.sqrt(head_dim)
         self._lib = load()
         self._c = PdByteCache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
@@ -85,15 +86,17 @@ class ByteCache:
         return self
 
     # -- what every call checks --------------------------------------------------
+    # (a call is bound by the host: it costs 6-8 us, of which these are two)
     def _data(self, name, t, shape):
-        """Pointer and strides of a tensor [req][token or row][head][dim] whose dims lie together."""
-        if t.shape != shape or t.device != self.device or t.dtype not in _TYPES:
+        """Pointer, strides and type of a tensor [req][token or row][head][dim] whose dims lie together."""
+        kind = _TYPES.get(t.dtype)
+        if kind is None or t.shape != shape or t.device != self.device:
             raise PdError(f"{name} must be float32, bfloat16 or float16 {shape} on {self.device}, not {t.dtype} "
                           f"{tuple(t.shape)} on {t.device}")
-        st = t.stride()
-        if st[3] != 1:
+        request, row, head, one = t.stride()
+        if one != 1:
             raise PdError(f"the dims of {name} must lie together")
-        return t.data_ptr(), _I64x3(st[0], st[1], st[2])
+        return t.data_ptr(), _I64x3(request, row, head), kind
 
     def _ints(self, name, t, shape, dtype=torch.int32):
         if t is None:
@@ -104,12 +107,14 @@ class ByteCache:
         return t.data_ptr()
 
     def _call(self, function, *args):
-        index = self.device.index
+        index = self._index
         if index == _current_device():
-            _check(function(self._p, *args, _raw_stream(index)))
+            rc = function(self._p, *args, _raw_stream(index))
         else:
             with torch.cuda.device(index):
-                _check(function(self._p, *args, _raw_stream(index)))
+                rc = function(self._p, *args, _raw_stream(index))
+        if rc:
+            _check(rc)
 
     # -- the operators -----------------------------------------------------------
     def append(self, k, v, lens, counts=None):
@@ -117,25 +122,28 @@ class ByteCache:
 
         lens: int32 [req], tokens of each request with the new ones; counts: int32 [req] or None, how many are new (None: all of
         k and v; fewer: the rest is padding).  A request whose numbers do not fit is left as it is."""
-        _require(k.dim() == 4, "k must be [req][new][head][dim], not %s", k.shape)
-        n_new = k.shape[1]
-        shape = (self.n_req, n_new, self.n_kv_head, self.head_dim)
-        kp, ks = self._data("k", k, shape)
-        vp, vs = self._data("v", v, shape)
-        dtype = k.dtype
-        _require(dtype == v.dtype, "k and v must have the same type, not %s and %s", dtype, v.dtype)
-        self._call(self._lib.pd_byte_append, kp, vp, _TYPES[dtype], ks, vs, n_new,
-                   self._ints("counts", counts, (self.n_req,)), self._ints("lens", lens, (self.n_req,)))
+        shape = k.shape
+        if len(shape) != 4:
+            raise PdError(f"k must be [req][new][head][dim], not {tuple(shape)}")
+        n_req, n_new = self.n_req, shape[1]
+        shape = (n_req, n_new, self.n_kv_head, self.head_dim)
+        kp, ks, kind = self._data("k", k, shape)
+        vp, vs, kind_v = self._data("v", v, shape)
+        if kind != kind_v:
+            raise PdError(f"k and v must have the same type, not {k.dtype} and {v.dtype}")
+        self._call(self._lib.pd_byte_append, kp, vp, kind, ks, vs, n_new,
+                   None if counts is None else self._ints("counts", counts, (n_req,)), self._ints("lens", lens, (n_req,)))
 
     def read(self, lens, n_tok, first=None, dtype=torch.float32):
         """Keys and values [req][n_tok][head][dim] of tokens first[r] .. first[r] + n_tok - 1 (int32 [req]; None: from 0) as the
         values that they stand for; zeros where a request holds none."""
-        _require(n_tok >= 0, "n_tok must be >= 0, not %s", n_tok)
-        _require(dtype in _TYPES, "dtype must be float32, bfloat16 or float16, not %s", dtype)
-        both = torch.empty((2, self.n_req, n_tok, self.n_kv_head, self.head_dim), dtype=dtype, device=self.device)
-        k, v = both.unbind()
-        self._call(self._lib.pd_byte_read, self._ints("first", first, (self.n_req,)), n_tok,
-                   self._ints("lens", lens, (self.n_req,)), k.data_ptr(), v.data_ptr(), _TYPES[dtype])
+        kind, n_req = _TYPES.get(dtype), self.n_req
+        if n_tok < 0 or kind is None:
+            raise PdError(f"n_tok must be >= 0, not {n_tok}" if n_tok < 0 else
+                          f"dtype must be float32, bfloat16 or float16, not {dtype}")
+        k, v = self.k_tail.new_empty((2, n_req, n_tok, self.n_kv_head, self.head_dim), dtype=dtype).unbind()
+        self._call(self._lib.pd_byte_read, None if first is None else self._ints("first", first, (n_req,)), n_tok,
+                   self._ints("lens", lens, (n_req,)), k.data_ptr(), v.data_ptr(), kind)
         return k, v
 
     def attention(self, q, lens, row_limit=None, key_tag=None, row_tag=None, scale=None, max_len=0, with_lse=False):
@@ -146,21 +154,23 @@ class ByteCache:
         [req][n_block * 64]) at most row_tag (int32 [req][row]); one that sees nothing gives zeros.  head: a multiple of the
         key heads, each of which serves the query heads in turn.  scale: 1 / sqrt(dim) unless given.  max_len: a number that
         no entry of lens exceeds, if known (shorter launches)."""
-        _require(q.dim() == 4, "q must be [req][row][head][dim], not %s", q.shape)
-        n_req, device = self.n_req, self.device
-        _, rows, heads, _ = q.shape
-        qp, qs = self._data("q", q, (n_req, rows, heads, self.head_dim))
+        shape = q.shape
+        if len(shape) != 4:
+            raise PdError(f"q must be [req][row][head][dim], not {tuple(shape)}")
+        n_req = self.n_req
+        _, rows, heads, _ = shape
+        qp, qs, kind = self._data("q", q, (n_req, rows, heads, self.head_dim))
         need = self._lib.pd_byte_attention_workspace_bytes(self._p, heads, rows, max_len)
         if need == 0:
             raise PdError(f"invalid attention: {self._lib.pd_last_error().decode()}")
-        out = torch.empty((n_req, rows, heads, self.head_dim), dtype=q.dtype, device=device)
-        lse = torch.empty((n_req, rows, heads), dtype=torch.float32, device=device) if with_lse else None
+        out = q.new_empty(shape)
+        lse = q.new_empty((n_req, rows, heads), dtype=torch.float32) if with_lse else None
         # of the caller's stream, or of the graph that captures it: never shared by two calls that may overlap
-        work = torch.empty(need, dtype=torch.uint8, device=device) if need > 16 else None
-        self._call(self._lib.pd_byte_attention, qp, _TYPES[q.dtype], qs, heads, rows, self._ints("lens", lens, (n_req,)),
-                   self._ints("row_limit", row_limit, (n_req, rows)),
-                   self._ints("key_tag", key_tag, (n_req, self.n_block * BLOCK), torch.uint16),
-                   self._ints("row_tag", row_tag, (n_req, rows)),
+        work = q.new_empty(need, dtype=torch.uint8) if need > 16 else None
+        self._call(self._lib.pd_byte_attention, qp, kind, qs, heads, rows, self._ints("lens", lens, (n_req,)),
+                   None if row_limit is None else self._ints("row_limit", row_limit, (n_req, rows)),
+                   None if key_tag is None else self._ints("key_tag", key_tag, (n_req, self.n_block * BLOCK), torch.uint16),
+                   None if row_tag is None else self._ints("row_tag", row_tag, (n_req, rows)),
                    self._scale if scale is None else scale, max_len, out.data_ptr(),
-                   lse.data_ptr() if with_lse else None, work.data_ptr() if work is not None else None, need)
+                   None if lse is None else lse.data_ptr(), None if work is None else work.data_ptr(), need)
         return (out, lse) if with_lse else out

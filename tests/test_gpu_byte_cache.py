@@ -446,6 +446,59 @@ def test_plain_tensors_go_in_and_come_out(dim):
             assert (got[r, n:] == 0).all()
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_tokens_and_queries_that_repeat_along_an_axis(kind):
+    """Strides of zero: one token for all heads, one prompt for all requests, one query for all rows and heads."""
+    x, _ = data(91, 1, 150, 1, 64, kind)
+    for shown in (x.expand(2, 150, 3, 64), x[:, :1].expand(2, 150, 3, 64)):
+        caches = [cache_of(2, 3, 64, 200) for _ in range(2)]
+        caches[0].append(shown, -shown, ints([150, 150]))
+        caches[1].append(shown.contiguous(), (-shown).contiguous(), ints([150, 150]))
+        q = x[:, 3:4].expand(2, 20, 6, 64)
+        outs = [c.attention(y, ints([150, 149]), with_lse=True) for c in caches for y in (q, q.contiguous())]
+        assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(outs[0], o))
+        assert all(torch.equal(a, b) for a, b in zip(*(c.read(ints([150, 150]), 150) for c in caches)))
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_lengths_beyond_what_there_is(rows):
+    """Lengths above the room count as the room, below zero as zero; what lies behind max_len may be left out, in whole blocks."""
+    k, _ = data(92, 2, 256, 2, 64, "bf16")
+    cache = cache_of(2, 2, 64, 256)
+    cache.append(k, k, ints([256, 256]))
+    q, _ = data(93, 2, rows, 2, 64, "bf16")
+    want = cache.attention(q, ints([256, 256]))
+    for lens in ([257, 1 << 30], [256, (1 << 31) - 1]):
+        assert torch.equal(cache.attention(q, ints(lens)), want)
+        assert torch.equal(cache.read(ints(lens), 300)[0], cache.read(ints([256, 256]), 300)[0])
+    for lens in ([-1, -(1 << 31)], [0, -64]):
+        out, lse = cache.attention(q, ints(lens), with_lse=True)
+        assert (out == 0).all() and torch.isneginf(lse).all() and (cache.read(ints(lens), 70)[1] == 0).all()
+    assert torch.equal(cache.attention(q, ints([256, 200]), max_len=100), cache.attention(q, ints([128, 128]), max_len=128))
+    limit = torch.full((2, rows), 1 << 30, dtype=torch.int32, device=DEV)
+    assert torch.equal(cache.attention(q, ints([256, 256]), row_limit=limit), want)
+    assert (cache.attention(q, ints([256, 256]), row_limit=-limit) == 0).all()
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_tags_at_the_ends_of_their_range(rows):
+    k, _ = data(94, 1, 130, 1, 32, "bf16")
+    cache = cache_of(1, 1, 32, 192)
+    cache.append(k, k, ints([130]))
+    q, _ = data(95, 1, rows, 1, 32, "bf16")
+    tags = np.full((1, 192), 65535, dtype=np.uint16)
+    tags[:, :70] = 32768
+    tags = torch.from_numpy(tags).to(DEV)
+
+    def seen(tag):
+        return cache.attention(q, ints([130]), key_tag=tags, row_tag=torch.full((1, rows), tag, dtype=torch.int32, device=DEV))
+    everything, first = cache.attention(q, ints([130])), cache.attention(q, ints([130]), row_limit=torch.full((1, rows), 70, dtype=torch.int32, device=DEV))
+    for tag, want in ((65535, everything), ((1 << 31) - 1, everything), (65534, first), (32768, first)):
+        assert torch.equal(seen(tag), want), tag
+    for tag in (32767, 0, -1, -(1 << 31)):
+        assert (seen(tag) == 0).all(), tag
+
+
 def test_refusals_of_the_binding():
     from paper_2506_23431_amd import ByteCache, PdError
     cache = cache_of(2, 2, 64, 128)

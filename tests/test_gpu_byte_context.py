@@ -221,3 +221,15 @@ def test_refusals():
         dec.use_byte_context()
     assert dec.lib.pd_byte_context(dec.ctx, C.c_void_p(256), 1 << 30, None) == -1
     dec.close()
+
+
+def test_an_encoder_decoder_context_refuses():
+    import ctypes as C
+    from paper_2506_23431_amd import PdError
+    from test_gpu_encdec import CASES as MODELS, make
+    _, _, dec = make(MODELS["encdec-sequential"])
+    with pytest.raises(PdError, match="decoder-only"):
+        dec.use_byte_context()
+    assert dec.lib.pd_byte_context(dec.ctx, C.c_void_p(256), 1 << 30, None) == -1
+    dec.use_byte_context(False)
+    dec.close()
