@@ -1247,7 +1247,7 @@ int byte_context_attention(pd_ctx *c, const LayerPtrs &lw, int A, int nreq, int 
   const int tail = c->L % BYTE_BLOCK + c->S * (c->M + 1) / 2;
   const int64_t units = (int64_t)nreq * a.nqg * g.n_head;
   PD_REQUIRE(units <= c->part_units, PD_EINVAL, "too many (request, head, query group) units: %lld", (long long)units);
-  const ByteAttnShape shape = byte_attn_shape(16, units, a.nblk + (tail + 31) / 32, g.head_dim);
+  const ByteAttnShape shape = byte_attn_shape(16, units, a.nblk + (tail + 31) / 32, g.head_dim, 4.0);
   a.nsplit = c->opt_splits > 0 ? c->opt_splits : shape.splits;
   a.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(a.nsplit, c->part_units / units));
   *splits = a.nsplit;

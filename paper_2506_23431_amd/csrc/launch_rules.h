@@ -360,20 +360,27 @@ struct ByteAttnShape { int tiles, groups, splits, waves; };
 // cols: query vectors per key head; heads: requests x key heads; nblk: blocks of 64 tokens.
 // Two tiles share the conversion of the values (us with one / with two: 16 heads, 2048 rows, 6144 tokens of size 128 158 / 118, 8 heads
 // and requests, 999 columns, 1500 tokens of 64 17.4 / 14.7).
-// Eight waves, and the tokens split over as many work-groups as there are compute units where that saves a wave enough blocks: a
-// block costs 0.0175 us per dim (one unit, 16 / 63 blocks without splits: size 128 8.4 / 21.5 us, 64 6.8 / 15.1), the launch that
-// joins the splits 3.5 us (no split / best split: 12 units of size 128, 16 blocks 10.2 / 9.4, 63 blocks 23.4 / 11.3; 32 units, 63 blocks
-// 24.5 / 13.6, 256 blocks 78 / 26; 4 units of size 64, 16 blocks 7.4 / 7.6).  Four waves where there is no more than a block for each
-// (12 units, 2 blocks 7.4 against 7.6), and where more units than compute units keep the chip busy with less left over at each
-// end (1024 units, 5 / 16 / 32 blocks 26 / 47 / 87 against 38 / 54 / 95; 63 blocks 161 against 159).
-inline ByteAttnShape byte_attn_shape(int cols, int64_t heads, int nblk, int head_dim) {
+// Eight waves, and the tokens split over as many work-groups, within the compute units, as cost least: a wave takes 0.0177 us per dim
+// and block, a work-group adds 1 / 150 of that to what all wait for (partial results, places in the caches), and the launch that
+// joins k splits takes 2.4 + 0.05 k us, 4.0 among the launches of a decode step (12 units of size 64, 25 blocks: with its merge 11.1 us whole,
+// 12.0 in four) (fitted to 194 times of up to 64 units, off by 5 %).  One unit, 16 / 63 blocks without splits: size 128
+// 8.4 / 21.5 us, 64 6.8 / 15.1.  No split / the best count: 12 units of size 128, 16 blocks 10.2 / 10.1, 63 blocks 23.4 / 11.3; 32 units, 63
+// blocks 24.5 / 13.6, 256 blocks 78 / 26.  As many as fit / as the same blocks per wave need: 16 units, 133 blocks of size 128 (16 / 9 splits)
+// 17.7 / 15.6, 4 units, 313 blocks (39 / 20) 14.7 / 13.6; one split more for half of the blocks per wave: 16 units, 71 blocks (8 / 9) 13.2 / 11.6.
+// Four waves where there is no more than a block for each (12 units, 2 blocks 7.4 against 7.6), and where more units than compute
+// units keep the chip busy with less left over at each end (1024 units, 5 / 16 / 32 blocks 26 / 47 / 87 against 38 / 54 / 95; 63 blocks 161
+// against 159).
+inline ByteAttnShape byte_attn_shape(int cols, int64_t heads, int nblk, int head_dim, double join_us = 2.4) {
   ByteAttnShape s{cols > 16 ? 2 : 1, 0, 1, 8};
   s.groups = (cols + 16 * s.tiles - 1) / (16 * s.tiles);
   const int64_t units = heads * s.groups;
   if (units < 1) return s;
-  const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / units, nblk / 8));
-  const int saved = (nblk + 7) / 8 - (nblk + 8 * splits - 1) / (8 * splits);
-  if (saved * 0.0175 * head_dim * s.tiles > 3.5) s.splits = splits;
   if (nblk <= 4 || (units > 256 && (nblk < 64 || s.tiles > 1))) s.waves = 4;
+  const int most = s.waves == 8 ? (int)std::min<int64_t>(256 / units, (nblk + 7) / 8) : 1;
+  double least = 1e30;
+  for (int k = 1; k <= std::max(most, 1); ++k) {
+    const double cost = (nblk + 8 * k - 1) / (8 * k) * s.tiles + units * k / 150. + (k > 1 ? (join_us + 0.05 * k) / (0.0177 * head_dim) : 0.);
+    if (cost < least) { least = cost; s.splits = k; }
+  }
   return s;
 }
