@@ -311,6 +311,7 @@ struct ByteAttnArgs {
   float *lse;                         // [req][row][head] or NULL
   float *part;
   int n_row, group, nqg, qt, nsplit, nblk; // group: query heads per key head; nqg: groups of 16 qt (row, query head) columns
+  int q_wide;                              // queries lie at multiples of 16 bytes
   float scale_log2, scale_low;             // log2(e) times the scale, and what its rounding left
   // CTX: a decode step over a decoder's context.  Rows and queries are the step's (fragments of high and low halves), the first
   // nblk blocks of the context are codes, everything behind them lies in the decoder's own cache of halves.
@@ -380,9 +381,6 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 // 4 x 32 heads, up to 5000 tokens 24.5 us and 4.0 for the merge (bf16).  Few short heads are a chain of trips to memory: 12 heads of
 // 64, 1000 tokens 7 us, of which an empty launch is 2.3.  Pieces of a prompt are bound by what a SIMD issues: 2048 rows of 16 heads of
 // 128 over 6144 tokens 118 us, 727 TFLOP/s, vector instructions 62 % and matrix instructions 27 % of the time with little overlap.
-// Work-groups of 128 columns that share the values' and keys' conversion to halves through LDS (a third fewer vector instructions)
-// take 114 us, halves of their waves in turn on the two kinds of instructions included, and 34 against 14.7 for 8 heads and requests of
-// 999 columns: not kept.
 // PP: probabilities as pairs of halves (22 bits): fp32 outputs need them, and half outputs are rounded as finely as single
 // probabilities would be (error of the whole 1.3 times the output's rounding without).
 // CTX: the columns are a decode step's rows, which see the context up to their limit and generated tokens by their tags.  32 tokens
@@ -949,6 +947,324 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   }
 }
 
+// Pieces of a prompt with half queries.  A work-group of 8 waves takes 128 columns, 32 a wave; each half of its waves takes every
+// other block.  A half's waves share the conversion of its blocks: codes become halves in LDS, in operand order, one step ahead (keys) or
+// behind (values) of the scores.  Half queries are exact in steps of a power of two (what lies 2^-22 below the row's largest is rounded to
+// 2^-33 of it), so that scores are one product of halves, added up in fp32, where the kernel above has three products of bytes and
+// puts whole numbers together.  While one half of the waves multiplies and converts, the other one has its softmax: a barrier
+// between the two keeps them apart.  Everything behind the scores is as above, the tail one more step of the first half.
+// us, the kernel above / this one: 16 heads of 128, 2048 rows, 6144 tokens 201 / 150; 2 requests, 8 key heads with 4 query heads each, 512
+// rows, 3000 tokens 113 / 84; 4 x 16 heads of 64, 512 rows, 2048 tokens 51 / 41; 28 x 8 heads of 128, 100 rows, 1000 tokens 54 / 42.  bf16
+// queries, of two bytes, gain next to nothing (125 / 122, 76 / 69, 85 / 86) and stay above.
+template <int HD>
+__global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
+  typedef f16_t T;
+  constexpr int NS = HD / 32, NT = HD / 16, ITEMS = HD * 4, IT = (ITEMS + 255) / 256;      // 16-byte loads of a block, per thread
+  constexpr float SLACK = slack_of(true), P_BITS = 15.f - SLACK;
+  __shared__ uint4 sm[2][2][2][HD * 8];                  // [step & 1][half][keys, values][fragments of 64 lanes]
+  __shared__ int sm_end[8];
+  __shared__ float sm_m[4][2][16], sm_l[4][2][16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int cw = wave & 3, half = wave >> 2, tid = threadIdx.x & 255;
+  const int rest = blockIdx.x >> 3, qg = a.nqg - 1 - rest % a.nqg, unit = rest / a.nqg * 8 + (blockIdx.x & 7);   // (as above)
+  if (unit >= a.c.n_req * a.c.n_kv_head) return;
+  const int h = unit % a.c.n_kv_head, req = unit / a.c.n_kv_head, n_cols = a.n_row * a.group, col0 = qg * 128 + cw * 32;
+  const size_t rhz = unit;
+
+  // ---- requests ----
+  const uint4 *K = (const uint4 *)(a.c.k + rhz * a.c.n_block * BYTE_BLOCK * HD);
+  const uint4 *V = (const uint4 *)(a.c.v + rhz * a.c.n_block * BYTE_BLOCK * HD);
+  int zero;
+  asm("v_mov_b32 %0, 0" : "=v"(zero));
+  const float *KS = a.c.k_scale + rhz * a.c.n_block + zero, *VS = a.c.v_scale + rhz * a.c.n_block + zero;
+  const uint16_t *TG = a.key_tag ? a.key_tag + (size_t)req * a.c.n_block * BYTE_BLOCK + 4 * g : nullptr;
+  const int b_last = a.c.n_block - 1;
+  uint4 rk[IT], rv[IT];
+  auto load_keys = [&](int b) {                          // (blocks that are not there: the last one's place)
+    const size_t at = (size_t)min(b, b_last) * ITEMS;
+#pragma unroll
+    for (int it = 0; it < IT; ++it) rk[it] = K[at + (ITEMS % 256 == 0 || tid + it * 256 < ITEMS ? tid + it * 256 : 0)];
+  };
+  auto load_values = [&](int b) {
+    const size_t at = (size_t)min(b, b_last) * ITEMS;
+#pragma unroll
+    for (int it = 0; it < IT; ++it) rv[it] = V[at + (ITEMS % 256 == 0 || tid + it * 256 < ITEMS ? tid + it * 256 : 0)];
+  };
+  auto put_keys = [&](int buf) {
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int e = tid + it * 256;
+      if (ITEMS % 256 != 0 && e >= ITEMS) continue;
+      uint4 *kp = &sm[buf][half][0][((e >> 7) * 4 + ((e >> 4) & 3)) * 64 + ((e >> 6) & 1) * 32 + (e & 15)];
+      kp[0] = frag_of(rk[it].x, rk[it].y).u; kp[16] = frag_of(rk[it].z, rk[it].w).u;
+    }
+  };
+  auto put_values = [&](int buf) {
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int e = tid + it * 256, d = e % HD;
+      if (ITEMS % 256 != 0 && e >= ITEMS) continue;
+      uint4 *vp = &sm[buf][half][1][(d >> 4) * 128 + e / HD * 16 + (d & 15)];
+      vp[0] = frag_of(rv[it].x, rv[it].y).u; vp[64] = frag_of(rv[it].z, rv[it].w).u;
+    }
+  };
+  float ks_next, vs_next;
+  uint2 tg[4] = {make_uint2(0, 0), make_uint2(0, 0), make_uint2(0, 0), make_uint2(0, 0)};
+  auto load_scales = [&](int b) {
+    b = min(b, b_last);
+    ks_next = KS[b]; vs_next = VS[b];
+    if (TG) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) tg[t] = *(const uint2 *)(TG + (size_t)b * BYTE_BLOCK + 16 * t);
+    }
+  };
+  load_keys(half);
+  load_values(half);
+  load_scales(half);
+
+  // ---- queries and what the columns see ----
+  const int cap = a.c.n_block * BYTE_BLOCK, n_keys = min(max(a.lens[req], 0), cap);
+  Frag q[2][NS];
+  float qf[2];
+  int lim[2], tag[2], reach = 0, lim_all = 0x7fffffff, tag_all = 0x7fffffff;
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const int col = min(col0 + qt * 16 + n, n_cols - 1), row = a.group == 1 ? col : col / a.group;
+    const T *p = (const T *)a.q + req * a.q_req + row * a.q_row + (h * a.group + col - row * a.group) * a.q_head + 8 * g;
+    float x[NS][8];
+    if (a.q_wide)
+#pragma unroll
+      for (int c = 0; c < NS; ++c) load8<T, true>(p + c * 32, x[c]);
+    else
+#pragma unroll
+      for (int c = 0; c < NS; ++c) load8<T, false>(p + c * 32, x[c]);
+    int top = 0;
+#pragma unroll
+    for (int c = 0; c < NS; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, (int)(__float_as_uint(x[c][j]) & 0x7fffffffu));
+    top = fold32(fold16(top, Max()), Max());
+    const bool finite = top < 0x7f800000;
+    const int ex = finite ? max((top >> 23) - 127, -100) : 8;
+    const float down = __uint_as_float((uint32_t)(127 + 8 - ex) << 23) * (a.scale_log2 < 0.f ? -1.f : 1.f);
+    qf[qt] = finite ? __uint_as_float((uint32_t)(127 - 8 + ex) << 23) * fabsf(a.scale_log2) : __uint_as_float(0x7fc00000u);
+#pragma unroll
+    for (int c = 0; c < NS; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[qt][c].hh[j] = (f16_t)(x[c][j] * down);
+    const bool there = col0 + qt * 16 + n < n_cols;
+    lim[qt] = there ? n_keys : 0;
+    if (a.row_limit) lim[qt] = min(lim[qt], max(a.row_limit[(size_t)req * a.n_row + row], 0));
+    tag[qt] = a.key_tag ? a.row_tag[(size_t)req * a.n_row + row] : 0;
+    reach = max(reach, lim[qt]);
+    if (there) { lim_all = min(lim_all, lim[qt]); tag_all = min(tag_all, tag[qt]); }
+  }
+  reach = __builtin_amdgcn_readfirstlane(fold_row(reach, Max()));
+  lim_all = __builtin_amdgcn_readfirstlane(fold_row(lim_all, Min()));
+  tag_all = __builtin_amdgcn_readfirstlane(fold_row(tag_all, Min()));
+  const int whole = n_keys / BYTE_BLOCK, end = min((reach + BYTE_BLOCK - 1) / BYTE_BLOCK, a.nblk), mine = min(end, whole);
+  sm_end[wave] = end;
+  put_keys(0);
+  load_keys(half + 2);
+  __syncthreads();
+  const int end_all = __builtin_amdgcn_readfirstlane(max(max(sm_end[0], sm_end[1]), max(sm_end[2], sm_end[3])));
+  const int steps = (min(end_all, whole) + 1) / 2;
+
+  float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f}, vref = 0.f;
+  floatx4 o[2][NT];
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) o[qt][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  Frag ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones.hh[e] = (f16_t)1.f;
+
+  floatx4 s[2][4];
+  Frag ph[2][2], pl[2][2];
+  float alpha[2], inv_ratio;
+  auto scores = [&](int buf) {
+    const uint4 *kl = sm[buf][half][0] + lane;
+#pragma unroll
+    for (int c = 0; c < NS; ++c)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        Frag f;
+        f.u = kl[(c * 4 + t) * 64];
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt) s[qt][t] = mfma16h(f, q[qt][c], c ? s[qt][t] : floatx4{0.f, 0.f, 0.f, 0.f});
+      }
+  };
+  auto probabilities = [&](auto tail_, int kb, float ks, float vs) {
+    constexpr bool TAIL = decltype(tail_)::value;
+    const int key0 = kb * BYTE_BLOCK + 4 * g;            // element e: token key0 + 16 (e >> 2) + (e & 3)
+    auto key = [&](int e) { return key0 + 16 * (e >> 2) + (e & 3); };
+    union { uint2 u[4]; uint16_t s[16]; uint32_t w[8]; } tags;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) tags.u[t] = tg[t];
+    bool whole_seen = !TAIL && kb * BYTE_BLOCK + BYTE_BLOCK <= lim_all;
+    if (!TAIL && TG) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, max(tags.w[e] >> 16, tags.w[e] & 0xffff));
+      whole_seen = uniform(whole_seen && !__any((int)top > tag_all));
+    }
+    float grow = 1.f;
+    if (!TAIL && uniform(vs > vref || (vs * 4096.f < vref && vs > 0.f))) {
+      const float to = __uint_as_float((__float_as_uint(vs) + 0x7fffffu) & 0xff800000u);
+      grow = vref / to;
+      vref = to;
+    }
+    if (TAIL && vref == 0.f) vref = 1.f;
+    // (the reciprocal of a power of two)
+    const float ratio = TAIL || vs == 0.f ? 1.f : vs * __uint_as_float(0x7f000000u - __float_as_uint(vref)), inv = __builtin_amdgcn_rcpf(ratio);
+    inv_ratio = inv == inv ? inv : 1.f;
+    auto masked = [&]() {
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          s[qt][e >> 2][e & 3] = ((key(e) < lim[qt]) & ((int)tags.s[e] <= tag[qt])) ? s[qt][e >> 2][e & 3] : -INFINITY;
+    };
+    if (!whole_seen) masked();
+    float off[2], kf[2], down[2];
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      kf[qt] = qf[qt] * ks;
+      kf[qt] = kf[qt] == 0.f ? 1e-37f : kf[qt];
+      float mloc = s[qt][0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mloc = fmaxf(mloc, s[qt][e >> 2][e & 3]);
+      mloc = ceilf(fold32(fold16(mloc, Max()), Max()) * kf[qt]);
+      const float m_new = mloc > m_run[qt] + SLACK ? mloc : m_run[qt], m_ref = m_new == -INFINITY ? 0.f : m_new;
+      alpha[qt] = __builtin_amdgcn_exp2f(m_run[qt] - m_ref);
+      down[qt] = alpha[qt] * grow;
+      m_run[qt] = m_new;
+      off[qt] = P_BITS - m_ref + lg2(ratio);
+    }
+    if (uniform(__any(down[0] != 1.f || down[1] != 1.f)))
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+        for (int i = 0; i < NT; ++i) o[qt][i] *= down[qt];
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[qt][e >> 2][e & 3] = fmaf(s[qt][e >> 2][e & 3], kf[qt], off[qt]);
+    if (!whole_seen && __any(kf[0] != kf[0] || off[0] != off[0] || kf[1] != kf[1] || off[1] != off[1])) masked();
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = __builtin_amdgcn_exp2f(s[qt][e >> 2][e & 3]);
+        ph[qt][e >> 3].hh[e & 7] = (f16_t)p;
+        pl[qt][e >> 3].hh[e & 7] = (f16_t)(p - (float)ph[qt][e >> 3].hh[e & 7]);
+      }
+  };
+  auto outputs = [&](auto tail_, int buf) {
+    constexpr bool TAIL = decltype(tail_)::value;
+    const uint4 *vl = sm[buf][half][1] + lane;
+    float take[2];
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      floatx4 t = mfma16h(ones, ph[qt][0], floatx4{0.f, 0.f, 0.f, 0.f});
+      t = mfma16h(ones, ph[qt][1], t);
+      t = mfma16h(ones, pl[qt][0], t);
+      t = mfma16h(ones, pl[qt][1], t);
+      l_run[qt] = fmaf(t[0], inv_ratio, l_run[qt] * alpha[qt]);
+      take[qt] = t[0];
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      Frag v0, v1;
+      v0.u = vl[i * 128]; v1.u = vl[i * 128 + 64];
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+        floatx4 t = mfma16h(v0, ph[qt][0], TAIL ? floatx4{0.f, 0.f, 0.f, 0.f} : o[qt][i]);
+        t = mfma16h(v1, ph[qt][1], t);
+        t = mfma16h(v0, pl[qt][0], t);
+        t = mfma16h(v1, pl[qt][1], t);
+        if (!TAIL) o[qt][i] = t;
+        else
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[qt][i][e] = take[qt] != 0.f ? fmaf(t[e], 1.f / vref, o[qt][i][e]) : o[qt][i][e];
+      }
+    }
+  };
+  if (half == 1) __syncthreads();
+  bool held = false;                                     // probabilities of the step before
+  for (int step = 0; step < steps; ++step) {
+    const int kb = 2 * step + half;
+    if (held) outputs(std::false_type(), (step + 1) & 1);
+    if (kb < mine) scores(step & 1);
+    put_values(step & 1);
+    put_keys((step + 1) & 1);
+    load_values(kb + 2);
+    load_keys(kb + 4);
+    __syncthreads();
+    if (kb < mine) probabilities(std::false_type(), kb, ks_next, __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(vs_next))));
+    held = kb < mine;
+    load_scales(kb + 2);
+    __syncthreads();
+  }
+  if (held) outputs(std::false_type(), (steps + 1) & 1);
+  if (half == 0) __syncthreads();
+  if (end_all > whole) {                                 // the tail, by the waves of the first half
+    __syncthreads();
+    const uint4 *kt = (const uint4 *)a.c.k_tail + (rhz * 2 + (whole & 1)) * (HD * 8);
+    const uint4 *vt = (const uint4 *)a.c.v_tail + (rhz * 2 + (whole & 1)) * (HD * 8);
+    for (int e = threadIdx.x; e < HD * 8; e += 512) {
+      sm[0][0][0][((e >> 8) * 4 + ((e >> 4) & 3)) * 64 + ((e >> 6) & 3) * 16 + (e & 15)] = kt[e];
+      const int d = e % HD, sg = e / HD;                 // slots without a token hold anything: zeros instead
+      Frag v;
+      v.u = vt[e];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (whole * BYTE_BLOCK + 16 * (2 * (sg >> 2) + (j >> 2)) + 4 * (sg & 3) + (j & 3) >= n_keys) v.hh[j] = (f16_t)0.f;
+      sm[0][0][1][(d >> 4) * 128 + (sg >> 2) * 64 + (sg & 3) * 16 + (d & 15)] = v.u;
+    }
+    __syncthreads();
+    if (half == 0 && end > whole) {
+      load_scales(whole);                                // (the tags)
+      scores(0);
+      probabilities(std::true_type(), whole, 1.f, 1.f);
+      outputs(std::true_type(), 0);
+    }
+  }
+  __syncthreads();
+
+  // ---- the halves' states become one ----
+  floatx4 *sm_o = (floatx4 *)sm;
+  if (half == 1) {
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      if (g == 0) { sm_m[cw][qt][n] = m_run[qt]; sm_l[cw][qt][n] = l_run[qt]; }
+#pragma unroll
+      for (int i = 0; i < NT; ++i) sm_o[((cw * 2 + qt) * NT + i) * 64 + lane] = o[qt][i] * vref;
+    }
+  }
+  __syncthreads();
+  if (half == 1) return;
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const float m1 = sm_m[cw][qt][n], M = fmaxf(m_run[qt], m1);
+    // (a half whose keys are all NaN has no maximum but a sum)
+    const float f0 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[qt] - M), f1 = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m1 - M);
+    const float L = f0 * l_run[qt] + f1 * sm_l[cw][qt][n];
+    const int col = col0 + qt * 16 + n;
+    if (col >= n_cols) continue;
+    const size_t at = ((size_t)req * a.n_row + col / a.group) * a.c.n_kv_head * a.group + h * a.group + col % a.group;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    if (a.lse && g == 0) a.lse[at] = (M + (__builtin_amdgcn_logf(L) - P_BITS)) * 0.6931471805599453f;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      floatx4 y = f0 * (o[qt][i] * vref) + f1 * sm_o[((cw * 2 + qt) * NT + i) * 64 + lane];
+      y *= inv;
+      store4((T *)a.out + at * HD + i * 16 + 4 * g, y);
+    }
+  }
+}
+
 // The splits of a unit become one: a block per (unit, 16-dim tile), wave w takes the splits w, w + 4, ...
 template <typename T, int HD, bool PP>
 __global__ __launch_bounds__(256) void k_byte_merge(ByteAttnArgs a) {
@@ -1146,10 +1462,24 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
   a.c = view(cache); a.q = q; a.q_req = q_strides[0]; a.q_row = q_strides[1]; a.q_head = q_strides[2];
   a.lens = lens; a.row_limit = row_limit; a.key_tag = key_tag; a.row_tag = row_tag; a.out = out; a.lse = out_lse;
   a.part = (float *)workspace; a.n_row = n_row; a.group = n_head / cache->n_kv_head;
-  a.nqg = sh.nqg; a.qt = sh.qt; a.nsplit = sh.nsplit; a.nblk = sh.nblk; 
+  a.nqg = sh.nqg; a.qt = sh.qt; a.nsplit = sh.nsplit; a.nblk = sh.nblk;
   a.scale_log2 = (float)(scale * 1.4426950408889634);
   a.scale_low = (float)(std::abs(scale * 1.4426950408889634) - std::abs((double)a.scale_log2));
+  a.q_wide = (((uintptr_t)q | (uint64_t)((q_strides[0] | q_strides[1] | q_strides[2]) * es)) & 15) == 0;
   hipStream_t s = (hipStream_t)hip_stream;
+  if (type == PD_TYPE_F16 && byte_attn_pieces(n_row * a.group, (int64_t)cache->n_req * cache->n_kv_head)) {
+    a.nqg = (n_row * a.group + 127) / 128;
+    const int64_t work_groups = ((int64_t)cache->n_req * cache->n_kv_head + 7) / 8 * 8 * a.nqg;
+    if ((rc = check_grid(work_groups))) return rc;
+    switch (cache->head_dim) {
+      case 32: hipLaunchKernelGGL(k_byte_piece<32>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
+      case 64: hipLaunchKernelGGL(k_byte_piece<64>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
+      case 96: hipLaunchKernelGGL(k_byte_piece<96>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
+      default: hipLaunchKernelGGL(k_byte_piece<128>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
+    }
+    PD_CHECK_HIP(hipGetLastError());
+    return PD_OK;
+  }
   const unsigned grid = (unsigned)sh.grid, tiles = (unsigned)(sh.units * sh.qt * (cache->head_dim / 16));
 #define PD_ATTEND_QT(T, HDV, QT, NW) \
   hipLaunchKernelGGL((k_byte_attn<T, HDV, !std::is_same<T, bf16_t>::value, QT, NW>), dim3(grid), dim3(64 * NW), 0, s, a)

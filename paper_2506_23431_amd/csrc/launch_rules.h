@@ -384,3 +384,11 @@ inline ByteAttnShape byte_attn_shape(int cols, int64_t heads, int nblk, int head
   }
   return s;
 }
+
+// Whether a piece of a prompt with half queries goes to work-groups of 128 columns (k_byte_piece), one to a compute unit: where they have
+// enough columns and fill every round of the 256 compute units but for an eighth (us, 32 columns to a wave / 128 to a work-group: 224 of them
+// 85 / 68, 256 201 / 150, 512 143 / 114; 64 48 / 100, 128 86 / 102, 384 146 / 148).
+inline bool byte_attn_pieces(int cols, int64_t heads) {
+  const int64_t groups = heads * ((cols + 127) / 128), rounds = (groups + 255) / 256;
+  return cols > 96 && groups * 8 >= rounds * 256 * 7;
+}

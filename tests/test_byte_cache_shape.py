@@ -15,6 +15,7 @@ extern "C" void shape(int cols, int64_t heads, int nblk, int head_dim, int *out)
   const ByteAttnShape s = byte_attn_shape(cols, heads, nblk, head_dim);
   out[0] = s.tiles; out[1] = s.groups; out[2] = s.splits; out[3] = s.waves;
 }
+extern "C" int pieces(int cols, int64_t heads) { return byte_attn_pieces(cols, heads); }
 """
 # head size, heads x requests, blocks of 64 tokens; us per launch (and its merge) by (waves, splits), bf16, one row
 MEASURED = [
@@ -56,10 +57,13 @@ def shape(tmp_path_factory):
                            "-o", str(d / "s.so")])
     lib = C.CDLL(str(d / "s.so"))
 
+    lib.pieces.argtypes = [C.c_int, C.c_int64]
+
     def call(cols, heads, nblk, head_dim):
         out = (C.c_int * 4)()
         lib.shape(cols, C.c_int64(heads), nblk, head_dim, out)
         return tuple(out)
+    call.pieces = lib.pieces
     return call
 
 
@@ -77,3 +81,20 @@ def test_shapes_hold_what_there_is(shape):
         assert groups * 16 * tiles >= cols > (groups - 1) * 16 * tiles or cols == groups == 0
         assert waves in (4, 8) and tiles == (1 if cols <= 16 else 2)
         assert splits == 1 or (splits * heads * groups <= 256 and (splits - 1) * 8 < nblk and waves == 8)
+
+
+# columns, heads x requests, us of half queries with 32 columns to a wave and with work-groups of 128
+PIECES = [(2048, 16, 212.07, 159.67), (1024, 16, 86.25, 101.91), (512, 16, 47.88, 100.09), (2048, 16, 121.11, 88.39),
+          (512, 64, 51.32, 41.54), (2048, 24, 145.57, 148.43), (256, 16, 53.05, 192.41), (128, 16, 33.42, 191.33)]
+
+
+@pytest.mark.parametrize("cols,heads,small,large", PIECES)
+def test_pieces_go_where_they_are_faster(shape, cols, heads, small, large):
+    assert bool(shape.pieces(cols, heads)) == (large < small)
+
+
+def test_pieces_need_no_workspace(shape):
+    for cols, heads in itertools.product((97, 128, 200, 1000, 5000, 1 << 20), (1, 7, 28, 56, 224, 1000, 1 << 16)):
+        if shape.pieces(cols, heads):
+            assert shape(cols, heads, 1 << 20, 128)[2] == 1
+    assert not shape.pieces(96, 1 << 20) and not shape.pieces(0, 256) and shape.pieces(97, 224) and not shape.pieces(97, 223)

@@ -256,6 +256,46 @@ def test_attention_subsequences_limits_and_rows_that_see_nothing(dim, kind):
                                                               [65534, 65535, 1, 0, 65536, 2]]), seed=2)
 
 
+LENS28 = [0, 1, 2, 31, 63, 64, 65, 90, 127, 128, 129, 130, 150, 190, 191, 192, 193, 200, 255, 256, 257, 320, 333, 64, 5, 128, 448, 100]
+
+
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+@pytest.mark.parametrize("rows,heads,kv,strided", [(100, 8, 8, False), (130, 4, 4, True), (50, 24, 8, False)])
+def test_attention_pieces_that_fill_the_chip(dim, rows, heads, kv, strided):
+    """Half queries, 128 columns to a work-group: ragged requests, causal limits with rows that see nothing, grouped heads."""
+    limits = [[max(n - rows + i + 1 - 3 * (r % 2), 0) for i in range(rows)] for r, n in enumerate(LENS28)]
+    check_attention("f16", LENS28, rows, heads, kv, dim, row_limit=limits, strided=strided, seed=dim, room=70)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_pieces_that_fill_the_chip_by_tags(dim):
+    rows, rng = 100, np.random.default_rng(8)
+    tags = [[int(x) for x in np.sort(rng.integers(0, 5, max(n, 1)))] for n in LENS28]
+    check_attention("f16", LENS28, rows, 8, 8, dim, tags=(tags, [[i % 6 - 1 for i in range(rows)] for _ in LENS28]), scale=-0.2, seed=3)
+    check_attention("f16", [200] * 28, rows, 8, 8, dim, max_len=230, seed=4)
+
+
+def test_attention_pieces_that_fill_the_chip_keep_nan_where_it_is():
+    k, _ = data(96, 28, 190, 8, 64, "f16")
+    q, _ = data(97, 28, 100, 8, 64, "f16")
+    limit = ints([[64 if i < 30 else 128 if i < 60 else 190 for i in range(100)]] * 28)
+    lens, out = ints([190] * 28), []
+    for bad in (False, True):
+        kk, vv, qq = k.clone(), k.flip(1).contiguous(), q.clone()
+        if bad:
+            kk[3, 100, 2, 5] = vv[4, 70, 1, 7] = vv[5, 150, 0, 9] = qq[6, 40, 3, 1] = float("nan")
+            qq[7, 50, 4, 2] = float("inf")
+        cache = cache_of(28, 8, 64, 200)
+        cache.append(kk, vv, lens)
+        out.append(cache.attention(qq, lens, row_limit=limit))
+    moved = (out[0] != out[1]).any(dim=3)
+    want = torch.zeros_like(moved)
+    want[3, 30:, 2] = want[4, 30:, 1] = want[5, 60:, 0] = want[6, 40, 3] = want[7, 50, 4] = True
+    assert torch.equal(moved, want)
+    assert torch.isnan(out[1][3, 30:, 2]).all() and torch.isnan(out[1][6, 40, 3]).all() and torch.isnan(out[1][7, 50, 4]).all()
+    assert torch.isnan(out[1][5, 60:, 0, 9]).all()
+
+
 def test_attention_few_rows_of_long_caches_are_split():
     check_attention("f32", [5000, 3], 2, 2, 2, 128, seed=4)
     check_attention("bf16", [9000], 8, 4, 4, 64, seed=5)
