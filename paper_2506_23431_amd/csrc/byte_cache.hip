@@ -116,8 +116,9 @@ __global__ __launch_bounds__(256, 3) void k_byte_store(StoreArgs a) {
   int u = blockIdx.x;                                    // heads first: their rows lie together
   const int h = u % a.c.n_kv_head; u /= a.c.n_kv_head;
   const int kind = u & 1, i0 = (u >> 1) % a.span, req = (u >> 1) / a.span;
-  const int count = a.counts ? a.counts[req] : a.n_new, len = a.lens[req], before = len - count;
-  if (count <= 0 || count > a.n_new || before < 0 || (int64_t)len > (int64_t)a.c.n_block * BYTE_BLOCK) return;
+  const int count = a.counts ? a.counts[req] : a.n_new, len = a.lens[req];
+  if (!byte_append_fits(len, count, a.n_new, a.c.n_block)) return;
+  const int before = len - count;
   const int first = before / BYTE_BLOCK, last = (len - 1) / BYTE_BLOCK;      // touched blocks
   const bool part = len % BYTE_BLOCK != 0;               // the last one stays in the tail
   // A last block with the first one's slot in the tail is stored by the work-group that has read that slot.

@@ -1,5 +1,5 @@
-// Launch shapes that follow from sizes alone: host code without device types, so that it can be compiled and checked by
-// itself.
+// Launch shapes that follow from sizes alone, and the kernels' own decisions on numbers that only the device has (constexpr): code
+// without device types, so that it can be compiled and checked by itself.
 #pragma once
 #include <stddef.h>
 #include <stdint.h>
@@ -350,6 +350,13 @@ inline RowTiling row_tiling(int n_tiles, int KT, int rows, int max_slices, bool 
       if (us < least) { least = us; best = RowTiling{costs[i].cut, costs[i].rt, costs[i].nt, ks}; }
     }
   return best;
+}
+
+// Whether a request's new tokens can be stored in the 8-bit cache: `count` of them, at most n_new, of `len` in all with them, in
+// n_block blocks of 64.  The device's numbers are anything: they are compared before anything is taken off them (a difference
+// of 32 bits turns round where a length is within the count of -2^31, and that request would pass for one of 2^31 tokens).
+constexpr bool byte_append_fits(int32_t len, int32_t count, int32_t n_new, int32_t n_block) {
+  return count >= 1 && count <= n_new && len >= count && len <= (int64_t)n_block * 64;
 }
 
 // ---------------------------------------------------------------------------

@@ -1,0 +1,21 @@
+"""The operators over the 8-bit cache at the ends of what their arguments may be, against tests/byte_cache_util.py."""
+
+import pytest
+
+from test_gpu_byte_cache import cache_of, data, ints
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("counts", [None, [70, 69, 1, 64, 5, 33]])
+def test_lengths_at_the_end_of_their_range_store_nothing(counts):
+    """Lengths within the count of -2^31, whose difference has no 32 bits."""
+    low = -(1 << 31)
+    k, _ = data(7, 6, 70, 2, 32, "f32")
+    for lens in ([low] * 6, [low + 1] * 6, [low + (70 if counts is None else c) - 1 for c in counts or [0] * 6]):
+        cache = cache_of(6, 2, 32, 128)
+        buffers = (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.k_tail, cache.v_tail)
+        was = [t.clone() for t in buffers]
+        cache.append(k, k, ints(lens), counts=None if counts is None else ints(counts))
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(was, buffers)), lens
