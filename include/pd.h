@@ -410,10 +410,10 @@ int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, int n_tok, co
  * Scores are products of whole numbers, exact: codes as they are, queries in steps of the row's largest / 32512 (bf16) or of at
  * most its 2^-21 (fp32, half), so at most half of that off; against the tail's halves, queries are halves (fp32: pairs of them).
  * (Pieces of a prompt of half queries that fill the chip: products of halves with the codes too, added up in fp32.)
- * Probabilities are rounded to halves (relative 2^-12; fp32 and half queries: pairs of halves, 2^-22; parts below 2^-35 of the
- * row's largest get lost), and so counted in out_lse; sums and the running maximum are fp32.  Infinities and NaN in tokens that a
- * row does not see do not reach it, save that a NaN reaches every row that sees any token of its block; of a query, they reach
- * its own row. */
+ * Probabilities are rounded to halves (relative 2^-12; fp32 and half queries: pairs of halves, 2^-22; parts below 2^-29, for
+ * pairs 2^-33, of the row's largest get lost), and so counted in out_lse; sums and the running maximum are fp32.  Infinities and
+ * NaN in tokens that a row does not see do not reach it, save that a NaN reaches every row that sees any token of its block; of a
+ * query, they reach its own row. */
 size_t pd_byte_attention_workspace_bytes(const pd_byte_cache *cache, int n_head, int n_row, int max_len);
 int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const int64_t *q_strides, int n_head, int n_row,
                       const int32_t *lens, const int32_t *row_limit, const uint16_t *key_tag, const int32_t *row_tag,

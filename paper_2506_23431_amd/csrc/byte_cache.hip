@@ -374,8 +374,8 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 //  * Values become halves in registers, exactly, once for QT tiles of 16 columns.
 //  * A block's key scale multiplies its scores.  The reference of the exponentials is a whole number (a running maximum rounded
 //    up), so that taking it off rounds nothing and rescaling by its change is exact.
-//  * A block's value scale multiplies its probabilities, over a power of two (vref) within 2^12 of it: the outputs add up in
-//    the matrix instruction, in units of vref, and are rescaled, exactly, in the rare case that it moves.
+//  * A block's value scale multiplies its probabilities, over a power of two (vref) within 4 times it: the outputs add up in
+//    the matrix instruction, in units of vref, and are rescaled, exactly, where it moves (rare: scales of neighbouring blocks are alike).
 //  * The sums of the probabilities are a product with ones: the same roundings as in the outputs, and no work for the vector
 //    units.
 // Measured: 32 requests, 4 query heads to each of 8 key heads, up to 8192 tokens of size 128 70 us, 4.9 TB/s (half queries); 16 rows of
@@ -779,9 +779,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     // ---- probabilities ----
     const float vs = TAIL ? 1.f : __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(vsc)));
-    // vref, a power of two, is kept within 1 and 2^12 of the scales (the outputs then stay below 2^15 127 2^41 times the tokens)
+    // vref, a power of two, is kept within 1 and 4 of the scales, so that the ratio takes at most 2 bits of the probabilities' room
+    // (with a ratio of 2^-11.5, tokens of 2^-13 of the row's largest would be off by up to 2.8e-4 as pairs of halves and 4.5e-3 as
+    // single ones, all alike, in the outputs and in the sums).  Moving it is exact: outputs stay below 2^15 127 times the tokens, in
+    // units of the largest vref that there was.
     float grow = 1.f;
-    if (!TAIL && uniform(vs > vref || (vs * 4096.f < vref && vs > 0.f))) {
+    if (!TAIL && uniform(vs > vref || (vs * 4.f < vref && vs > 0.f))) {
       const float to = __uint_as_float((__float_as_uint(vs) + 0x7fffffu) & 0xff800000u);
       grow = vref / to;
       vref = to;
@@ -1111,7 +1114,7 @@ __global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
       whole_seen = uniform(whole_seen && !__any((int)top > tag_all));
     }
     float grow = 1.f;
-    if (!TAIL && uniform(vs > vref || (vs * 4096.f < vref && vs > 0.f))) {
+    if (!TAIL && uniform(vs > vref || (vs * 4.f < vref && vs > 0.f))) {
       const float to = __uint_as_float((__float_as_uint(vs) + 0x7fffffu) & 0xff800000u);
       grow = vref / to;
       vref = to;
