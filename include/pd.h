@@ -359,7 +359,9 @@ int pd_get_info(pd_ctx *ctx, int key, void *hip_stream, int64_t *value);
  * All arrays are contiguous.  Codes and tails lie in the order in which the attention kernel loads them: the 64 tokens of a block
  * by groups of 16 (tail: 8) dims for keys; for values by 4 groups g of 16 tokens, place i of which is token 16 (i >> 2) + 4 g +
  * (i & 3) (tail: two halves, s, of 8 places, token 16 (2 s + (i >> 2)) + 4 g + (i & 3)).  Who fills a cache in another way than
- * through pd_byte_append keeps codes within [-127, 127], scales at 0 or above, and codes of 0 where the scale is 0. */
+ * through pd_byte_append keeps codes within [-127, 127], scales at 0 or within [2^-32, 2^32] (append's lie within 2^-31 and 2^10;
+ * attention adds blocks up in units that follow their value scales, and further apart they pass what fp32 holds), and codes of 0
+ * where the scale is 0. */
 #define PD_BYTE_BLOCK 64
 #define PD_TYPE_F32  0
 #define PD_TYPE_BF16 1

@@ -67,7 +67,7 @@ class ByteCache:
     @classmethod
     def from_tensors(cls, k, v, k_scale, v_scale, k_tail, v_tail):
         """A cache that holds what these tensors hold (the ones of to_tensors, on its device; copied).  Codes are within
-        [-127, 127], and 0 where the scale is 0; scales are not negative."""
+        [-127, 127], and 0 where the scale is 0; scales are 0 or within [2^-32, 2^32]."""
         _require(k.dim() == 5 and k.shape[3] == BLOCK, "k must be [req][head][block][%d][dim], not %s", BLOCK, tuple(k.shape))
         r, h, n, _, d = k.shape
         for name, t, shape, dtype in (("k", k, k.shape, torch.int8), ("v", v, (r, h, n, d, BLOCK), torch.int8),

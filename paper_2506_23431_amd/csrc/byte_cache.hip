@@ -781,8 +781,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     const float vs = TAIL ? 1.f : __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(vsc)));
     // vref, a power of two, is kept within 1 and 4 of the scales, so that the ratio takes at most 2 bits of the probabilities' room
     // (with a ratio of 2^-11.5, tokens of 2^-13 of the row's largest would be off by up to 2.8e-4 as pairs of halves and 4.5e-3 as
-    // single ones, all alike, in the outputs and in the sums).  Moving it is exact: outputs stay below 2^15 127 times the tokens, in
-    // units of the largest vref that there was.
+    // single ones, all alike, in the outputs and in the sums).  Moving it is exact: outputs stay below 2^15 127 2^30 (tokens) times
+    // the largest vref there was over the present one, which is 2^64 at most as scales lie within 2^-32 and 2^32.
     float grow = 1.f;
     if (!TAIL && uniform(vs > vref || (vs * 4.f < vref && vs > 0.f))) {
       const float to = __uint_as_float((__float_as_uint(vs) + 0x7fffffu) & 0xff800000u);

@@ -148,3 +148,22 @@ def test_stored_tokens_of_magnitudes_that_lie_apart(kind, order):
     cache.append(*(torch.from_numpy(x).to(DEV).expand(1, n, heads, dim) for x in (k, v)), ints([n]))
     q, qn = queries(kind, 1, 3, heads, dim, n)
     check(kind, cache, q, qn, n, {(0, 63): [u.contents(x[0])[3] for x in (k, v)]})
+
+
+@pytest.mark.parametrize("rows", [4, 40])
+@pytest.mark.parametrize("kind,least,most", [("f32", -32, 32), ("bf16", -32, 32), ("f16", -32, 8)])
+@pytest.mark.parametrize("order", ["up", "down", "mixed"])
+def test_scales_at_the_ends_of_their_range(kind, least, most, order, rows):
+    """Value scales of 2^-32 and 2^32 (half: what it holds) in one cache: rows that see all of it, and rows that see a half."""
+    n, heads = 2048, 64
+    scales = np.array(apart(order, most - least, n // 64)) / 0.7 * 2.0 ** most
+    plain = plain_cache(1, 1, heads, 64, scales, k_scale=np.where(np.arange(n // 64) % 2, 2.0 ** -32, 2.0 ** 32))
+    q, qn = queries(kind, 1, rows, heads, 64, n)
+    seen = int(np.flatnonzero(plain["k"][0, 0].any(axis=(1, 2)))[0])       # the block of the token whose key is not 0
+    down = 2.0 ** -7 / float(plain["k_scale"][0, 0, seen])
+    if kind == "f16":                            # (queries stay halves)
+        plain["k_scale"][:] = 2.0 ** -7
+    else:
+        q, qn = q * down, qn * down
+    limits = [n if i % 2 else n // 2 for i in range(rows)]
+    check(kind, made(plain), q, qn, n, {(0, h): held(plain, 0, h) for h in (0, 40)}, limits=limits)
