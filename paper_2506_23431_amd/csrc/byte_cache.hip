@@ -364,7 +364,7 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(intx4, a), __builtin_bit_cast(intx4, b), c, 0, 0, 0);
 }
 
-// grid: (split, group of 16 QT columns, key head, request); NW waves.  The blocks of 64 tokens of a (request, key head) are dealt
+// grid: (split, group of 16 QT columns, key head, request), dealt by byte_attn_group; NW waves.  The blocks of 64 tokens of a (request, key head) are dealt
 // round-robin to the waves of its splits.  A column is one query vector (row, query head of the key head's group).  Scores come
 // out of the matrix instruction with a lane holding 16 tokens of one column, which are its operand for the outputs as they are:
 // element e of step s of group g is token 32 s + 16 (e >> 2) + 4 g + (e & 3) of the block.
@@ -401,16 +401,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   __shared__ float sm_m[QT][NW][16], sm_l[QT][NW][16];
   __shared__ floatx4 sm_o[NW][NT][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  int u = blockIdx.x, split = 0, qg, unit;
-  if (a.nqg > 1) {                                       // column groups of one (request, head) on one XCD, whose cache they share
-    const int xcd = u & 7, rest = u >> 3;
-    qg = a.nqg - 1 - rest / a.nsplit % a.nqg;            // (the last rows of a causal piece have the most to do)
-    split = rest % a.nsplit;
-    unit = rest / a.nsplit / a.nqg * 8 + xcd;
-    if (unit >= a.c.n_req * a.c.n_kv_head) return;
-  } else {
-    split = u % a.nsplit; unit = u / a.nsplit; qg = 0;
-  }
+  const ByteGroup me = byte_attn_group(blockIdx.x, a.c.n_req * a.c.n_kv_head, a.nqg, a.nsplit);
+  const int unit = me.unit, split = me.split, qg = a.nqg - 1 - me.group;      // (the last rows of a causal piece have the most to do)
   const int h = unit % a.c.n_kv_head, reqi = unit / a.c.n_kv_head, req = CTX ? a.req0 + reqi : reqi;
   const int n_cols = a.n_row * a.group;
   const size_t rhz = CTX ? (size_t)req * a.c.n_kv_head + h : (size_t)unit;
@@ -970,8 +962,8 @@ __global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
   __shared__ float sm_m[4][2][16], sm_l[4][2][16];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int cw = wave & 3, half = wave >> 2, tid = threadIdx.x & 255;
-  const int rest = blockIdx.x >> 3, qg = a.nqg - 1 - rest % a.nqg, unit = rest / a.nqg * 8 + (blockIdx.x & 7);   // (as above)
-  if (unit >= a.c.n_req * a.c.n_kv_head) return;
+  const ByteGroup me = byte_attn_group(blockIdx.x, a.c.n_req * a.c.n_kv_head, a.nqg, 1);
+  const int unit = me.unit, qg = a.nqg - 1 - me.group;   // (as above)
   const int h = unit % a.c.n_kv_head, req = unit / a.c.n_kv_head, n_cols = a.n_row * a.group, col0 = qg * 128 + cw * 32;
   const size_t rhz = unit;
 
@@ -1433,7 +1425,7 @@ static int byte_shape(const pd_byte_cache *c, int n_head, int n_row, int max_len
   out->qt = sh.tiles; out->waves = sh.waves; out->nsplit = sh.splits;
   out->nqg = sh.groups;
   out->units = heads * sh.groups;
-  out->grid = (out->nqg > 1 ? (heads + 7) / 8 * 8 * out->nqg : out->units) * out->nsplit;
+  out->grid = out->units * out->nsplit;
   return check_grid(std::max(out->grid, out->units * out->qt * (c->head_dim / 16)));
 }
 
@@ -1473,7 +1465,7 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
   hipStream_t s = (hipStream_t)hip_stream;
   if (type == PD_TYPE_F16 && byte_attn_pieces(n_row * a.group, (int64_t)cache->n_req * cache->n_kv_head)) {
     a.nqg = (n_row * a.group + 127) / 128;
-    const int64_t work_groups = ((int64_t)cache->n_req * cache->n_kv_head + 7) / 8 * 8 * a.nqg;
+    const int64_t work_groups = (int64_t)cache->n_req * cache->n_kv_head * a.nqg;
     if ((rc = check_grid(work_groups))) return rc;
     switch (cache->head_dim) {
       case 32: hipLaunchKernelGGL(k_byte_piece<32>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
@@ -1585,7 +1577,7 @@ int byte_context_attention(pd_ctx *c, const LayerPtrs &lw, int A, int nreq, int 
   a.nsplit = c->opt_splits > 0 ? c->opt_splits : shape.splits;
   a.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(a.nsplit, c->part_units / units));
   *splits = a.nsplit;
-  const int64_t grid = (a.nqg > 1 ? ((int64_t)nreq * g.n_head + 7) / 8 * 8 * a.nqg : units) * a.nsplit;
+  const int64_t grid = units * a.nsplit;
   int rc = check_grid(grid);
   if (rc) return rc;
 #define PD_CONTEXT(HDV)                                                                                                       \
