@@ -1187,7 +1187,9 @@ __global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
       }
     }
   };
-  if (half == 1) __syncthreads();
+  // (one barrier more for one half here, for the other one at the end: both pass as many.  The branch is the wave's own, and nothing in
+  // LDS waits for these two.)
+  if (half == 1) __builtin_amdgcn_s_barrier();
   bool held = false;                                     // probabilities of the step before
   for (int step = 0; step < steps; ++step) {
     const int kb = 2 * step + half;
@@ -1204,7 +1206,7 @@ __global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
     __syncthreads();
   }
   if (held) outputs(std::false_type(), (steps + 1) & 1);
-  if (half == 0) __syncthreads();
+  if (half == 0) __builtin_amdgcn_s_barrier();
   if (end_all > whole) {                                 // the tail, by the waves of the first half
     __syncthreads();
     const uint4 *kt = (const uint4 *)a.c.k_tail + (rhz * 2 + (whole & 1)) * (HD * 8);
