@@ -409,9 +409,9 @@ int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, int n_tok, co
  *   out_lse    fp32 [n_req][n_row][n_head] or NULL: log(sum_j exp(scale q.k_j)), -infinity for a row that sees nothing
  *   workspace  at least pd_byte_attention_workspace_bytes (same arguments; 0: they are invalid), 16-byte aligned; it holds
  *              nothing between calls, and calls that may overlap need one each
- * Scores are products of whole numbers, exact: codes as they are, queries in steps of the row's largest / 32512 (bf16) or of at
- * most its 2^-21 (fp32, half), so at most half of that off; against the tail's halves, queries are halves (fp32: pairs of them).
- * (Pieces of a prompt of half queries that fill the chip: products of halves with the codes too, added up in fp32.)
+ * Scores are products of whole numbers, exact: codes as they are, queries in steps of at most 2^-21 of the row's largest, so at
+ * most half of that off; against the tail's halves, queries are halves (fp32: pairs of them).  (Pieces of a prompt of bf16 or half
+ * queries that fill the chip: products of halves with the codes too, added up in fp32.)
  * Probabilities are rounded to halves (relative 2^-12; fp32 and half queries: pairs of halves, 2^-22; parts below 2^-29, for
  * pairs 2^-33, of the row's largest get lost), and so counted in out_lse; sums and the running maximum are fp32.  Infinities and
  * NaN in tokens that a row does not see do not reach it, save that a NaN reaches every row that sees any token of its block; of a

@@ -368,9 +368,10 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 // round-robin to the waves of its splits.  A column is one query vector (row, query head of the key head's group).  Scores come
 // out of the matrix instruction with a lane holding 16 tokens of one column, which are its operand for the outputs as they are:
 // element e of step s of group g is token 32 s + 16 (e >> 2) + 4 g + (e & 3) of the block.
-//  * Scores are products of bytes, exact in 32-bit integers: the keys' codes as they lie, queries as whole numbers of two bytes
-//    (bf16) or three (fp32, half), in steps of the row's largest / 32512 or of a power of two at most 2^-21 of it.  No key is
-//    converted.
+//  * Scores are products of bytes, exact in 32-bit integers: the keys' codes as they lie, queries as whole numbers of three bytes,
+//    in steps of a power of two at most 2^-21 of the row's largest.  No key is converted.  (Two bytes would be enough for bf16
+//    where a row's channels are alike, and 0.2-0.4 us less for a step, 10 % for a piece of a prompt; with one channel 1000 times the
+//    others they were off by 6 times the output's own rounding, and a decoder's logits by 4.5e-2 instead of 7e-4.)
 //  * Values become halves in registers, exactly, once for QT tiles of 16 columns.
 //  * A block's key scale multiplies its scores.  The reference of the exponentials is a whole number (a running maximum rounded
 //    up), so that taking it off rounds nothing and rescaling by its change is exact.
@@ -392,7 +393,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   constexpr int NS = HD / 32, NT = HD / 16;              // contraction steps of the scores, 16-dim tiles of the outputs
   constexpr int KW = HD / 64;                            // 16-byte loads per key and lane (8 bytes more where a step is left)
   constexpr int PSTR = HD + 2;
-  constexpr int NP = sizeof(T) == 2 && !PP ? 2 : 3, NC = (HD + 63) / 64;     // bytes of a query value; contraction steps of 64
+  constexpr int NP = 3, NC = (HD + 63) / 64;             // bytes of a query value; contraction steps of 64
   constexpr bool QP = sizeof(T) == 4 || CTX;
   constexpr float SLACK = slack_of(PP), P_BITS = 15.f - SLACK;
   __shared__ uint4 sm_qi[QT][NP][NC][64], sm_q[CTX ? 1 : QT][CTX ? 1 : (QP ? 2 : 1) * NS][64];
@@ -517,14 +518,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       const bool finite = top < 0x7f800000u;
       const int ex = finite ? max((int)(top >> 23) - 127, -100) : 8;
       const float down = __uint_as_float((uint32_t)(127 + 8 - ex) << 23);
-      // whole numbers up to 127 in their highest byte: two bytes as finely as they go, three by a power of two, which rounds
-      // nothing; the factor of a row that is not finite is NaN, and so are its scores
-      const float big = fmaxf(__uint_as_float(top), 1e-31f), sign = a.scale_log2 < 0.f ? -1.f : 1.f;   // (factors are not negative)
-      const float most = NP == 2 ? 127.f * 256.f / big : __uint_as_float((uint32_t)(127 + 21 - ex) << 23);
-      const float up = finite ? most * sign : 0.f;
+      // whole numbers of up to 2^22, by a power of two, which rounds nothing; the factor of a row that is not finite is NaN, and so
+      // are its scores
+      const float sign = a.scale_log2 < 0.f ? -1.f : 1.f;          // (factors are not negative)
+      const float up = finite ? __uint_as_float((uint32_t)(127 + 21 - ex) << 23) * sign : 0.f;
       if (pt == 0) {
-        sm_qf[qt][0][m] = !finite ? __uint_as_float(0x7fc00000u)
-                          : NP == 2 ? big / (127.f * 256.f) * fabsf(a.scale_log2) : __uint_as_float((uint32_t)(127 - 21 + ex) << 23);
+        sm_qf[qt][0][m] = !finite ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 - 21 + ex) << 23);
         sm_qf[qt][1][m] = __uint_as_float((uint32_t)(127 - 8 + ex) << 23) * fabsf(a.scale_log2);
       }
 #pragma unroll
@@ -734,26 +733,23 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     } else {
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        intx4 s[NP][4];
+        // the products of the highest byte, below 2^20, times 256 and those of the next one, added to them
+        intx4 s[2][4];
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int b = 0; b < NP; ++b)
 #pragma unroll
-          for (int b = 0; b < NP; ++b) {
+          for (int c = 0; c < NC; ++c) {
             const uint4 q = sm_qi[qt][b][c][lane];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              const intx4 from = c ? s[b][t] : intx4{0, 0, 0, 0};
+              const intx4 from = c ? s[b >> 1][t] : b == 1 ? s[0][t] << 8 : intx4{0, 0, 0, 0};
               // (the last 32 dims: half of the bytes are zeros, and the query's beside them anything.  The instruction for 32
               // would do half the work, but its sums right behind those of the one for 64, whose results it adds to, came out wrong.)
-              s[b][t] = mfma_codes(c < KW ? kw[t][c < KW ? c : 0] : make_uint4(kn[t].x, kn[t].y, 0, 0), q, from);
+              s[b >> 1][t] = mfma_codes(c < KW ? kw[t][c < KW ? c : 0] : make_uint4(kn[t].x, kn[t].y, 0, 0), q, from);
             }
           }
-        // (the products of the two highest bytes stay below 2^30)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float high = (float)((s[0][e >> 2][e & 3] << 8) + s[1][e >> 2][e & 3]);
-          sv[qt][e] = NP == 2 ? high : fmaf(high, 256.f, (float)s[NP - 1][e >> 2][e & 3]);
-        }
+        for (int e = 0; e < 16; ++e) sv[qt][e] = fmaf((float)s[0][e >> 2][e & 3], 256.f, (float)s[1][e >> 2][e & 3]);
         if (QT > 1) __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -790,7 +786,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
     for (int qt = 0; qt < QT; ++qt) {
       // fp32: the factor with what its roundings leave, which would shift a block's probabilities together
       float kf = TAIL ? sm_qf[qt][1][n] : qf[qt] * ks, kf_low = 0.f;
-      if (!TAIL && NP == 3) {
+      if (!TAIL) {
         const float f = qf[qt] * fabsf(a.scale_log2);
         kf = f * ks;
         if (sizeof(T) == 4) kf_low = fmaf(qf[qt] * a.scale_low, ks, fmaf(f, ks, -kf));
@@ -943,20 +939,18 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
   }
 }
 
-// Pieces of a prompt with half queries.  A work-group of 8 waves takes 128 columns, 32 a wave; each half of its waves takes every
+// Pieces of a prompt with bf16 or half queries.  A work-group of 8 waves takes 128 columns, 32 a wave; each half of its waves takes every
 // other block.  A half's waves share the conversion of its blocks: codes become halves in LDS, in operand order, one step ahead (keys) or
-// behind (values) of the scores.  Half queries are exact in steps of a power of two (what lies 2^-22 below the row's largest is rounded to
-// 2^-33 of it), so that scores are one product of halves, added up in fp32, where the kernel above has three products of bytes and
-// puts whole numbers together.  While one half of the waves multiplies and converts, the other one has its softmax: a barrier
-// between the two keeps them apart.  Everything behind the scores is as above, the tail one more step of the first half.
-// us, the kernel above / this one: 16 heads of 128, 2048 rows, 6144 tokens 201 / 150; 2 requests, 8 key heads with 4 query heads each, 512
-// rows, 3000 tokens 113 / 84; 4 x 16 heads of 64, 512 rows, 2048 tokens 51 / 41; 28 x 8 heads of 128, 100 rows, 1000 tokens 54 / 42.  bf16
-// queries, of two bytes, gain next to nothing (125 / 122, 76 / 69, 85 / 86) and stay above.
-template <int HD>
+// behind (values) of the scores.  As halves such queries are exact in steps of a power of two (what lies 2^-22 below the row's largest is
+// rounded to 2^-33 of it), so that scores are one product of halves, added up in fp32, where the kernel above has three products of
+// bytes and puts whole numbers together.  While one half of the waves multiplies and converts, the other one has its softmax: a
+// barrier between the two keeps them apart.  Everything behind the scores is as above, the tail one more step of the first half.
+// us, the kernel above / this one, half (bf16): 16 heads of 128, 2048 rows, 6144 tokens 160 / 148 (129 / 116); 4 x 16 heads of 64, 512 rows,
+// 2048 tokens without limits 51 / 41 (43 / 34); 28 x 8 heads of 128, 100 rows, 1000 tokens 45 / 41 (40 / 33), one block 19 / 12 (18 / 10).
+template <typename T, int HD, bool PP>
 __global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
-  typedef f16_t T;
   constexpr int NS = HD / 32, NT = HD / 16, ITEMS = HD * 4, IT = (ITEMS + 255) / 256;      // 16-byte loads of a block, per thread
-  constexpr float SLACK = slack_of(true), P_BITS = 15.f - SLACK;
+  constexpr float SLACK = slack_of(PP), P_BITS = 15.f - SLACK;
   __shared__ uint4 sm[2][2][2][HD * 8];                  // [step & 1][half][keys, values][fragments of 64 lanes]
   __shared__ int sm_end[8];
   __shared__ float sm_m[4][2][16], sm_l[4][2][16];
@@ -1154,7 +1148,7 @@ __global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
       for (int e = 0; e < 16; ++e) {
         const float p = __builtin_amdgcn_exp2f(s[qt][e >> 2][e & 3]);
         ph[qt][e >> 3].hh[e & 7] = (f16_t)p;
-        pl[qt][e >> 3].hh[e & 7] = (f16_t)(p - (float)ph[qt][e >> 3].hh[e & 7]);
+        if (PP) pl[qt][e >> 3].hh[e & 7] = (f16_t)(p - (float)ph[qt][e >> 3].hh[e & 7]);
       }
   };
   auto outputs = [&](auto tail_, int buf) {
@@ -1165,8 +1159,7 @@ __global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
     for (int qt = 0; qt < 2; ++qt) {
       floatx4 t = mfma16h(ones, ph[qt][0], floatx4{0.f, 0.f, 0.f, 0.f});
       t = mfma16h(ones, ph[qt][1], t);
-      t = mfma16h(ones, pl[qt][0], t);
-      t = mfma16h(ones, pl[qt][1], t);
+      if (PP) { t = mfma16h(ones, pl[qt][0], t); t = mfma16h(ones, pl[qt][1], t); }
       l_run[qt] = fmaf(t[0], inv_ratio, l_run[qt] * alpha[qt]);
       take[qt] = t[0];
     }
@@ -1178,8 +1171,7 @@ __global__ __launch_bounds__(512, 2) void k_byte_piece(ByteAttnArgs a) {
       for (int qt = 0; qt < 2; ++qt) {
         floatx4 t = mfma16h(v0, ph[qt][0], TAIL ? floatx4{0.f, 0.f, 0.f, 0.f} : o[qt][i]);
         t = mfma16h(v1, ph[qt][1], t);
-        t = mfma16h(v0, pl[qt][0], t);
-        t = mfma16h(v1, pl[qt][1], t);
+        if (PP) { t = mfma16h(v0, pl[qt][0], t); t = mfma16h(v1, pl[qt][1], t); }
         if (!TAIL) o[qt][i] = t;
         else
 #pragma unroll
@@ -1465,16 +1457,15 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
   a.scale_low = (float)(std::abs(scale * 1.4426950408889634) - std::abs((double)a.scale_log2));
   a.q_wide = (((uintptr_t)q | (uint64_t)((q_strides[0] | q_strides[1] | q_strides[2]) * es)) & 15) == 0;
   hipStream_t s = (hipStream_t)hip_stream;
-  if (type == PD_TYPE_F16 && byte_attn_pieces(n_row * a.group, (int64_t)cache->n_req * cache->n_kv_head)) {
+  if (type != PD_TYPE_F32 && byte_attn_pieces(n_row * a.group, (int64_t)cache->n_req * cache->n_kv_head)) {
     a.nqg = (n_row * a.group + 127) / 128;
     const int64_t work_groups = (int64_t)cache->n_req * cache->n_kv_head * a.nqg;
     if ((rc = check_grid(work_groups))) return rc;
-    switch (cache->head_dim) {
-      case 32: hipLaunchKernelGGL(k_byte_piece<32>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
-      case 64: hipLaunchKernelGGL(k_byte_piece<64>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
-      case 96: hipLaunchKernelGGL(k_byte_piece<96>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
-      default: hipLaunchKernelGGL(k_byte_piece<128>, dim3((unsigned)work_groups), dim3(512), 0, s, a); break;
-    }
+#define PD_PIECE(T, HDV) \
+  hipLaunchKernelGGL((k_byte_piece<T, HDV, std::is_same<T, f16_t>::value>), dim3((unsigned)work_groups), dim3(512), 0, s, a)
+    if (type == PD_TYPE_BF16) PD_BYTE_DIMS(bf16_t, cache->head_dim, PD_PIECE)
+    else PD_BYTE_DIMS(f16_t, cache->head_dim, PD_PIECE)
+#undef PD_PIECE
     PD_CHECK_HIP(hipGetLastError());
     return PD_OK;
   }

@@ -392,9 +392,12 @@ inline ByteAttnShape byte_attn_shape(int cols, int64_t heads, int nblk, int head
   return s;
 }
 
-// Whether a piece of a prompt with half queries goes to work-groups of 128 columns (k_byte_piece), one to a compute unit: where they have
-// enough columns and fill every round of the 256 compute units but for an eighth (us, 32 columns to a wave / 128 to a work-group: 224 of them
-// 85 / 68, 256 201 / 150, 512 143 / 114; 64 48 / 100, 128 86 / 102, 384 146 / 148).
+// Whether a piece of a prompt with bf16 or half queries goes to work-groups of 128 columns (k_byte_piece), one to a compute unit: where
+// they have enough columns and fill every round of the 256 compute units but for an eighth.  us, 32 columns to a wave / 128 to a
+// work-group: bf16, causal, 64 work-groups 36 / 79, 128 59 / 79, 192 74 / 80, 224 81.4 / 80.2, 256 129 / 116, 384 81 / 89 and 118 / 119, 480
+// 129 / 123, 576 108 / 107, 768 115 / 106; half 64 38 / 99, 192 91 / 102, 224 98 / 102, 256 160 / 148, 384 96 / 106, 576 129 / 127.  Neither length nor
+// head size moves the line: at 224 and 256, one block 0.54-0.64 of the time, four 0.7-0.85, 16 0.77-0.9, heads of 32 to 128; the one place
+// above it that loses more than 3 % is 1024 work-groups of halves over 200 tokens of 128 (67 / 76).
 inline bool byte_attn_pieces(int cols, int64_t heads) {
   const int64_t groups = heads * ((cols + 127) / 128), rounds = (groups + 255) / 256;
   return cols > 96 && groups * 8 >= rounds * 256 * 7;

@@ -12,6 +12,7 @@ CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
 SOURCE = r"""
 #include "launch_rules.h"
 extern "C" int append_fits(int len, int count, int n_new, int n_block) { return byte_append_fits(len, count, n_new, n_block); }
+extern "C" int pieces(int cols, int64_t heads) { return byte_attn_pieces(cols, heads); }
 extern "C" void one(int i, int heads, int groups, int splits, int *out) {
   const ByteGroup g = byte_attn_group(i, heads, groups, splits);
   out[0] = g.unit; out[1] = g.group; out[2] = g.split;
@@ -76,3 +77,21 @@ def test_large_launches_keep_their_parts(rules):
     for heads, groups, splits in ((1 << 26, 31, 1), (9, (1 << 31) // 9, 1), (1, (1 << 31) - 1, 1), (1, 1, 256), (8, 1, 16)):
         rules.one(heads * groups * splits - 1, heads, groups, splits, last)
         assert tuple(last) == (heads - 1, groups - 1, splits - 1), (heads, groups, splits)
+
+
+# columns, heads x requests, us with 32 columns to a wave and with work-groups of 128; type, head size, tokens, causal or not
+PIECES = [(512, 16, 35.6, 79.02, "bf16", 128, 4096, True), (1024, 16, 58.68, 79.04, "bf16", 128, 4096, True),
+          (1536, 16, 74.4, 79.85, "bf16", 128, 4096, True), (1792, 16, 81.43, 80.17, "bf16", 128, 4096, True),
+          (2048, 16, 129.34, 116.46, "bf16", 128, 6144, True), (1024, 48, 81.36, 89.16, "bf16", 64, 3000, True),
+          (256, 64, 22.25, 30.28, "bf16", 32, 2000, True), (1280, 48, 129.3, 122.84, "bf16", 128, 3000, True),
+          (100, 224, 17.69, 10.25, "bf16", 128, 64, False), (100, 224, 10.89, 6.39, "bf16", 32, 64, False),
+          (100, 224, 19.24, 13.39, "bf16", 96, 100, True), (200, 512, 502.26, 420.55, "bf16", 96, 6000, True),
+          (512, 64, 153.46, 120.32, "bf16", 128, 6000, False), (1536, 16, 90.67, 102.13, "f16", 128, 4096, True),
+          (2048, 16, 160.19, 148.21, "f16", 128, 6144, True), (1024, 48, 96.02, 106.12, "f16", 64, 3000, True),
+          (100, 224, 18.88, 12.03, "f16", 128, 64, False), (100, 224, 21.56, 18.29, "f16", 128, 256, True),
+          (100, 224, 27.98, 24.08, "f16", 32, 1000, True), (512, 64, 186.4, 151.82, "f16", 128, 6000, False)]
+
+
+@pytest.mark.parametrize("cols,heads,small,large", [x[:4] for x in PIECES], ids=["-".join(map(str, x[4:] + x[:2])) for x in PIECES])
+def test_pieces_of_every_length_and_head_size_go_where_they_are_faster(rules, cols, heads, small, large):
+    assert bool(rules.pieces(cols, C.c_int64(heads))) == (large < small)
