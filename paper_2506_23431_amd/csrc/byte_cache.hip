@@ -744,7 +744,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
             for (int t = 0; t < 4; ++t) {
               const intx4 from = c ? s[b >> 1][t] : b == 1 ? s[0][t] << 8 : intx4{0, 0, 0, 0};
               // (the last 32 dims: half of the bytes are zeros, and the query's beside them anything.  The instruction for 32
-              // would do half the work, but its sums right behind those of the one for 64, whose results it adds to, came out wrong.)
+              // would do half the work, but its sums right behind those of the one for 64, whose results it adds to, came out
+              // wrong.  Why is not known, and so the two never meet.)
               s[b >> 1][t] = mfma_codes(c < KW ? kw[t][c < KW ? c : 0] : make_uint4(kn[t].x, kn[t].y, 0, 0), q, from);
             }
           }
@@ -826,7 +827,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
       l_run[qt] = fmaf(t[0], inv_ratio == inv_ratio ? inv_ratio : 1.f, l_run[qt] * alpha);
       take[qt] = t[0];
       // (used here: sunk behind the branch below, the first use of the sums stood too close to the product for them to have
-      // arrived, where the branch is taken)
+      // arrived, where the branch is taken.  tests/test_byte_cache_code.py walks every path of the built kernels for such uses.)
       asm volatile("" : "+v"(l_run[qt]), "+v"(take[qt]));
       if (__any(down != 1.f))
 #pragma unroll
