@@ -353,8 +353,13 @@ int pd_get_info(pd_ctx *ctx, int key, void *hip_stream, int64_t *value);
  * slots (block b uses slot b mod 2).  A token is rounded to halves when it comes (magnitudes beyond 65504 saturate, NaN stays);
  * when its block is whole, scale = fp32(largest magnitude / 127), code = value / scale to the nearest whole number, ties to
  * even, and the token stands for code * scale from then on: at most half a scale from what came, plus the rounding to halves.
- * What a cache holds does not depend on the pieces in which its tokens came.  A NaN makes the scale of its block NaN, and with
- * it every key (or value) of the block.
+ * What a cache holds does not depend on the pieces in which its tokens came.  A NaN makes the scale of its block NaN, and with it
+ * every key (or value) of the block.
+ *
+ * `lens` is what a request holds, the number that its last pd_byte_append was given, and no bound on what is read (row_limit and
+ * n_tok are): a smaller one that ends inside a whole block looks for that block in the tail, where other tokens are by then, or
+ * none.  So tokens can be taken back, for all calls from then on, within the block that is not whole yet or to a multiple of
+ * PD_BYTE_BLOCK, and to nothing else.
  *
  * All arrays are contiguous.  Codes and tails lie in the order in which the attention kernel loads them: the 64 tokens of a block
  * by groups of 16 (tail: 8) dims for keys; for values by 4 groups g of 16 tokens, place i of which is token 16 (i >> 2) + 4 g +
@@ -400,7 +405,7 @@ int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, int n_tok, co
  * h / (n_head / n_kv_head).
  *   q          [n_req][n_row][n_head][head_dim] of one of the PD_TYPE_* types, by strides as in pd_byte_append (HOST array of
  *              three: request, row, head)
- *   lens       int32 [n_req]; beyond what the cache holds counts as full, negative as 0
+ *   lens       int32 [n_req], what is held, as above; beyond what the cache has room for counts as full, negative as 0
  *   row_limit  int32 [n_req][n_row] or NULL
  *   key_tag    uint16 [n_req][n_block * 64] and row_tag int32 [n_req][n_row], both or neither; key_tag 16-byte aligned
  *   max_len    HOST number that no entry of lens exceeds, for the shape of the launch (0: what the cache has room for); tokens
@@ -431,8 +436,9 @@ int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const
  * 768, 12 of 1024, 24 of 2048 move the logits by up to 7.6e-3, 8.8e-3, 1.8e-2 (rms 1.3e-3, 1.5e-3, 2.8e-3 of logits whose own is
  * 0.56, 0.64, 0.90).  Attention with its merge, us per layer, halves / codes: 12 heads of 64, 1 x 1024 tokens 9.8 / 11.1 (short
  * contexts lose), 16 heads of 64, 8 x 2048 tokens 18.2 / 15.7, 16 of 128, 1 x 8192 19.5 / 17.8, 32 of 128, 4 x 4096 70 / 58.
- *   dev_buffer  DEVICE, 256-byte aligned, at least pd_byte_context_bytes(ctx) (0: this context cannot have one), to outlive the
- *               ctx or the next such call; NULL: back to the 16-bit cache
+ *   dev_buffer  DEVICE, 256-byte aligned, at least pd_byte_context_bytes(ctx) (0: this context cannot have one), to outlive
+ *               every context pass and step that was enqueued, on any stream, before the next such call or pd_destroy (the call
+ *               itself waits for none of them); NULL: back to the 16-bit cache
  * Contexts that are encoded already get their codes at once, others at the end of pd_prefill_context; asynchronous on
  * hip_stream.  PD_OPT_PROFILE 1 and 2 bracket the kernel, and the pair, with events recorded beside them; 3 has no effect on it. */
 size_t pd_byte_context_bytes(const pd_ctx *ctx);

@@ -26,7 +26,8 @@ class ByteCache:
     """Keys and values of n_req requests with room for max_tokens tokens each; how they are held stands at pd_byte_cache.
 
     How many tokens a request holds is the caller's to know and is passed to every call as `lens`, an int32 tensor [n_req] on the
-    cache's device that is read when the kernels run.  Work is queued on the current stream of that device; nothing is kept
+    cache's device that is read when the kernels run: the numbers that the last append was given, not a bound on what is read (for
+    that there are row_limit, first and n_tok; a smaller number that ends inside a whole block finds other tokens there, or none).  Work is queued on the current stream of that device; nothing is kept
     between calls but the tensors k, v, k_scale, v_scale, k_tail, v_tail, and calls can be captured into a graph.  For inference:
     no gradients are recorded."""
 

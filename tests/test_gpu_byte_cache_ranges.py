@@ -19,3 +19,24 @@ def test_lengths_at_the_end_of_their_range_store_nothing(counts):
         was = [t.clone() for t in buffers]
         cache.append(k, k, ints(lens), counts=None if counts is None else ints(counts))
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(was, buffers)), lens
+
+
+@pytest.mark.parametrize("back", [201, 192, 128, 64, 0])
+def test_tokens_taken_back(back):
+    """Within the block that is not whole yet, or to whole blocks: what is left, and what comes after, is as if they had never been there."""
+    import numpy as np
+    from test_gpu_byte_cache import check_contents
+    k, kn = data(11, 2, 400, 2, 64, "f16")
+    q, _ = data(12, 2, 3, 2, 64, "f16")
+    cache, other = cache_of(2, 2, 64, 400), cache_of(2, 2, 64, 400)
+    cache.append(k[:, :215], k[:, :215], ints([215] * 2))
+    if back:
+        other.append(k[:, :back], k[:, :back], ints([back] * 2))
+    assert torch.equal(cache.attention(q, ints([back] * 2)), other.attention(q, ints([back] * 2)))
+    assert torch.equal(cache.read(ints([back] * 2), 220)[1], other.read(ints([back] * 2), 220)[1])
+    new = k[:, 300:400]
+    cache.append(new, new, ints([back + 100] * 2))
+    other.append(new, new, ints([back + 100] * 2))
+    for r in range(2):
+        check_contents(cache, r, *[np.concatenate([kn[r, :back], kn[r, 300:]])] * 2, back + 100)
+    assert torch.equal(cache.attention(q, ints([back + 100] * 2)), other.attention(q, ints([back + 100] * 2)))
