@@ -160,6 +160,8 @@ class ByteCache:
             raise PdError(f"q must be [req][row][head][dim], not {tuple(shape)}")
         n_req = self.n_req
         _, rows, heads, _ = shape
+        if max_len > self.n_block * BLOCK:                # (all there is room for; the C argument has 32 bits and no checks)
+            max_len = 0
         qp, qs, kind = self._data("q", q, (n_req, rows, heads, self.head_dim))
         need = self._lib.pd_byte_attention_workspace_bytes(self._p, heads, rows, max_len)
         if need == 0:

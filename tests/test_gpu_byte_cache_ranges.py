@@ -40,3 +40,14 @@ def test_tokens_taken_back(back):
     for r in range(2):
         check_contents(cache, r, *[np.concatenate([kn[r, :back], kn[r, 300:]])] * 2, back + 100)
     assert torch.equal(cache.attention(q, ints([back + 100] * 2)), other.attention(q, ints([back + 100] * 2)))
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_bound_on_the_lengths_that_32_bits_do_not_hold(rows):
+    k, _ = data(13, 1, 300, 1, 64, "bf16")
+    q, _ = data(14, 1, rows, 1, 64, "bf16")
+    cache = cache_of(1, 1, 64, 300)
+    cache.append(k, k, ints([300]))
+    want = cache.attention(q, ints([300]))
+    for bound in (300, 320, 321, (1 << 31) - 1, 1 << 31, (1 << 32) + 1, (1 << 32) + 64, 1 << 70):
+        assert torch.equal(cache.attention(q, ints([300]), max_len=bound), want), bound
