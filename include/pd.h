@@ -327,8 +327,8 @@ int pd_measure_read_bandwidth(const void *dev_buf, size_t buf_bytes, size_t chun
  *   PD_INFO_STREAM_LOADS    1, 2: decode steps use the non-temporal hint (the value of PD_OPT_STREAM_LOADS)
  *   PD_INFO_KEPT_BYTES      bytes of the weights of a decode step that keep ordinary loads while the others take the
  *                           hint (at most 210 MB; 0 without the hint)
- *   PD_INFO_BYTE_BLOCKS     blocks of 64 tokens of every request's context that decode steps read from 8-bit codes
- *                           (pd_byte_context; 0: none)
+ *   PD_INFO_BYTE_BLOCKS     blocks of 64 tokens of every request's context that decode steps read from 8-bit codes, in the
+ *                           layers that have them (pd_byte_context; 0: none, as where all layers keep pairs of halves)
  *   PD_INFO_KV_SATURATED    keys and values written since pd_create whose magnitude exceeded the
  *                           largest half (65504) and were stored as +-65504 (dtype 1 only; always
  *                           0 for dtype 0).  Non-zero means the 16-bit cache cannot represent

@@ -544,7 +544,11 @@ extern "C" int pd_get_info(pd_ctx *c, int key, void *hip_stream, int64_t *value)
     case PD_INFO_KV_PAIR_LAYERS: *value = c->pair_layers; return PD_OK;
     case PD_INFO_CONTEXT_PAIRS: *value = context_pairs(c) ? 1 : 0; return PD_OK;
     case PD_INFO_STREAM_LOADS: *value = c->stream_loads; return PD_OK;
-    case PD_INFO_BYTE_BLOCKS: *value = c->byte_context && c->prefilled ? c->L / PD_BYTE_BLOCK : 0; return PD_OK;
+    case PD_INFO_BYTE_BLOCKS: {
+      const bool any = std::any_of(c->layers.begin(), c->layers.end(), [](const LayerPtrs &lp) { return lp.b_k; });
+      *value = any && c->prefilled ? c->L / PD_BYTE_BLOCK : 0;
+      return PD_OK;
+    }
     case PD_INFO_KEPT_BYTES: *value = mfma_kept_bytes(c); return PD_OK;
     case PD_INFO_KV_SATURATED: {
       hipStream_t s = (hipStream_t)hip_stream;
