@@ -364,7 +364,7 @@ int pd_get_info(pd_ctx *ctx, int key, void *hip_stream, int64_t *value);
  * All arrays are contiguous.  Codes and tails lie in the order in which the attention kernel loads them: the 64 tokens of a block
  * by groups of 16 (tail: 8) dims for keys; for values by 4 groups g of 16 tokens, place i of which is token 16 (i >> 2) + 4 g +
  * (i & 3) (tail: two halves, s, of 8 places, token 16 (2 s + (i >> 2)) + 4 g + (i & 3)).  Who fills a cache in another way than
- * through pd_byte_append keeps codes within [-127, 127], scales at 0 or within [2^-32, 2^32] (append's lie within 2^-31 and 2^10;
+ * through pd_byte_append keeps codes within [-127, 127], tails finite (or NaN), scales at 0 or within [2^-32, 2^32] (append's lie within 2^-31 and 2^10;
  * attention adds blocks up in units that follow their value scales, and further apart they pass what fp32 holds), and codes of 0
  * where the scale is 0. */
 #define PD_BYTE_BLOCK 64
@@ -414,10 +414,10 @@ int pd_byte_read(const pd_byte_cache *cache, const int32_t *first, int n_tok, co
  *   out_lse    fp32 [n_req][n_row][n_head] or NULL: log(sum_j exp(scale q.k_j)), -infinity for a row that sees nothing
  *   workspace  at least pd_byte_attention_workspace_bytes (same arguments; 0: they are invalid), 16-byte aligned; it holds
  *              nothing between calls, and calls that may overlap need one each
- * Scores are products of whole numbers, exact: codes as they are, queries in steps of at most 2^-21 of the row's largest, so at
- * most half of that off; against the tail's halves, queries are halves (fp32: pairs of them).  (Pieces of a prompt of bf16 or half
+ * Scores are products of whole numbers, exact: codes as they are, queries in steps of at most 2^-21 of the row's largest (but not
+ * of less than 2^-121), so at most half of that off; against the tail's halves, queries are halves (fp32: pairs of them).  (Pieces of a prompt of bf16 or half
  * queries that fill the chip: products of halves with the codes too, added up in fp32.)
- * Probabilities are rounded to halves (relative 2^-12; fp32 and half queries: pairs of halves, 2^-22; parts below 2^-29, for
+ * Probabilities are rounded to halves (relative 2^-11; fp32 and half queries: pairs of halves, 2^-22; parts below 2^-29, for
  * pairs 2^-33, of the row's largest get lost), and so counted in out_lse; sums and the running maximum are fp32.  Infinities and
  * NaN in tokens that a row does not see do not reach it, save that a NaN reaches every row that sees any token of its block; of a
  * query, they reach its own row. */
@@ -432,10 +432,13 @@ int pd_byte_attention(const pd_byte_cache *cache, const void *q, int type, const
  * them (the rest of the context and all generated tokens) from the 16-bit cache, which the context pass and pd_teacher_forced
  * go on using for all of it: half of the bytes of the attention's hot loop for a further buffer.  Layers that keep pairs of halves
  * (kv_pair_layers) stay as they are.  A caller's trade, not the library's: keys and values of the context are off by up to half
- * a scale, 1/254 of their block's largest.  Measured against the same steps over the 16-bit cache, random tokens: 6 layers of width
- * 768, 12 of 1024, 24 of 2048 move the logits by up to 7.6e-3, 8.8e-3, 1.8e-2 (rms 1.3e-3, 1.5e-3, 2.8e-3 of logits whose own is
- * 0.56, 0.64, 0.90).  Attention with its merge, us per layer, halves / codes: 12 heads of 64, 1 x 1024 tokens 9.8 / 11.1 (short
- * contexts lose), 16 heads of 64, 8 x 2048 tokens 18.2 / 15.7, 16 of 128, 1 x 8192 19.5 / 17.8, 32 of 128, 4 x 4096 70 / 58.
+ * a scale, 1/254 of their block's largest, and queries meet them as whole numbers in steps of 2^-21 of a row's largest.  Measured
+ * against the same steps over the 16-bit cache, random tokens: 6 layers of width 768, 12 of 1024, 24 of 2048, 32 of 4096 move the
+ * logits by up to 7.6e-3, 8.8e-3, 1.8e-2, 3.2e-2 (rms 1.3e-3, 1.5e-3, 2.8e-3, 5.9e-3 of logits whose own is 0.56, 0.64, 0.90, 1.28): the
+ * deeper the model the more, and past what everything else here is held to (2e-2) at 32 layers.  ms per step, halves / codes, of
+ * these models with 1 x 1024, 8 x 2048, 1 x 8192, 4 x 4096 input tokens: 0.147 / 0.162 (short contexts lose), 0.581 / 0.553, 1.190 /
+ * 1.183, 5.79 / 5.31; attention with its merge, us per layer: 9.3 / 11.4, 18.3 / 16.0, 20.2 / 19.5, 61 / 45.  Filling the codes takes
+ * 0.03, 0.30, 0.65 and 2.7 ms of the context pass.
  *   dev_buffer  DEVICE, 256-byte aligned, at least pd_byte_context_bytes(ctx) (0: this context cannot have one), to outlive
  *               every context pass and step that was enqueued, on any stream, before the next such call or pd_destroy (the call
  *               itself waits for none of them); NULL: back to the 16-bit cache

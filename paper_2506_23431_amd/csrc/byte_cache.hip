@@ -371,7 +371,7 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 //  * Scores are products of bytes, exact in 32-bit integers: the keys' codes as they lie, queries as whole numbers of three bytes,
 //    in steps of a power of two at most 2^-21 of the row's largest.  No key is converted.  (Two bytes would be enough for bf16
 //    where a row's channels are alike, and 0.2-0.4 us less for a step, 10 % for a piece of a prompt; with one channel 1000 times the
-//    others they were off by 6 times the output's own rounding, and a decoder's logits by 4.5e-2 instead of 7e-4.)
+//    others outputs were off by 6 times what all other roundings explain, and a decoder's logits by 4.5e-2 instead of 7e-4.)
 //  * Values become halves in registers, exactly, once for QT tiles of 16 columns.
 //  * A block's key scale multiplies its scores.  The reference of the exponentials is a whole number (a running maximum rounded
 //    up), so that taking it off rounds nothing and rescaling by its change is exact.
@@ -380,9 +380,9 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 //  * The sums of the probabilities are a product with ones: the same roundings as in the outputs, and no work for the vector
 //    units.
 // Measured: 32 requests, 4 query heads to each of 8 key heads, up to 8192 tokens of size 128 70 us, 4.9 TB/s (half queries); 16 rows of
-// 4 x 32 heads, up to 5000 tokens 24.5 us and 4.0 for the merge (bf16).  Few short heads are a chain of trips to memory: 12 heads of
-// 64, 1000 tokens 7 us, of which an empty launch is 2.3.  Pieces of a prompt are bound by what a SIMD issues: 2048 rows of 16 heads of
-// 128 over 6144 tokens 118 us, 727 TFLOP/s, vector instructions 62 % and matrix instructions 27 % of the time with little overlap.
+// 4 x 32 heads, up to 5000 tokens 25 us and 4.1 for the merge (bf16).  Few short heads are a chain of trips to memory: 12 heads of
+// 64, 1000 tokens 7 us, of which an empty launch is 2.3.  Pieces of a prompt are bound by what a SIMD issues: fp32, 2048 rows of 16 heads
+// of 128 over 6144 tokens 183 us, 470 TFLOP/s.
 // PP: probabilities as pairs of halves (22 bits): fp32 outputs need them, and half outputs are rounded as finely as single
 // probabilities would be (error of the whole 1.3 times the output's rounding without).
 // CTX: the columns are a decode step's rows, which see the context up to their limit and generated tokens by their tags.  32 tokens
@@ -946,6 +946,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 // rounded to 2^-33 of it), so that scores are one product of halves, added up in fp32, where the kernel above has three products of
 // bytes and puts whole numbers together.  While one half of the waves multiplies and converts, the other one has its softmax: a
 // barrier between the two keeps them apart.  Everything behind the scores is as above, the tail one more step of the first half.
+// Bound by what a SIMD issues as well: bf16, 2048 rows of 16 heads of 128 over 6144 tokens 116 us, 745 TFLOP/s, vector instructions 58 %
+// and matrix instructions 38 % of the time.  Halves with heads of 128 keep nine registers in scratch memory (150 us).
 // us, the kernel above / this one, half (bf16): 16 heads of 128, 2048 rows, 6144 tokens 160 / 148 (129 / 116); 4 x 16 heads of 64, 512 rows,
 // 2048 tokens without limits 51 / 41 (43 / 34); 28 x 8 heads of 128, 100 rows, 1000 tokens 45 / 41 (40 / 33), one block 19 / 12 (18 / 10).
 template <typename T, int HD, bool PP>
@@ -1492,7 +1494,8 @@ extern "C" int pd_byte_attention(const pd_byte_cache *cache, const void *q, int 
 // a decoder's context
 // ---------------------------------------------------------------------------
 // One work-group per (request, head, block of the context, keys or values): halves of the decoder's cache (two of its blocks of 32
-// tokens), codes of this one.
+// tokens), codes of this one.  Bound by the bytes: 4 x 4096 tokens of 32 heads of 128 in 88 us a layer, 4.6 TB/s of the 4.9 that a copy
+// reaches; 8 x 2048 of 16 heads of 64 25 us, 1 x 8192 of 16 heads of 128 28, 1 x 1024 of 12 heads of 64 5.6.
 template <int HD>
 __global__ __launch_bounds__(256, 3) void k_byte_context(ByteCache c, const f16_t *kc, const f16_t *vc, int kv_cap, int n_whole) {
   constexpr int P = HD + 8;

@@ -365,18 +365,20 @@ constexpr bool byte_append_fits(int32_t len, int32_t count, int32_t n_new, int32
 struct ByteAttnShape { int tiles, groups, splits, waves; };
 
 // cols: query vectors per key head; heads: requests x key heads; nblk: blocks of 64 tokens.
-// Two tiles share the conversion of the values (us with one / with two: 16 heads, 2048 rows, 6144 tokens of size 128 158 / 118, 8 heads
-// and requests, 999 columns, 1500 tokens of 64 17.4 / 14.7).
+// Two tiles share the conversion of the values (us with one / with two, bf16 and fp32: 16 heads, 2048 rows, 6144 tokens of size 128
+// 170 / 131 and 218 / 180, 8 heads and requests, 999 columns, 1500 tokens of 64 69 / 65 and 91 / 87).
 // Eight waves, and the tokens split over as many work-groups, within the compute units, as cost least: a wave takes 0.0177 us per dim
 // and block, a work-group adds 1 / 150 of that to what all wait for (partial results, places in the caches), and the launch that
-// joins k splits takes 2.4 + 0.05 k us, 4.0 among the launches of a decode step (12 units of size 64, 25 blocks: with its merge 11.1 us whole,
-// 12.0 in four) (fitted to 194 times of up to 64 units, off by 5 %).  One unit, 16 / 63 blocks without splits: size 128
-// 8.4 / 21.5 us, 64 6.8 / 15.1.  No split / the best count: 12 units of size 128, 16 blocks 10.2 / 10.1, 63 blocks 23.4 / 11.3; 32 units, 63
-// blocks 24.5 / 13.6, 256 blocks 78 / 26.  As many as fit / as the same blocks per wave need: 16 units, 133 blocks of size 128 (16 / 9 splits)
-// 17.7 / 15.6, 4 units, 313 blocks (39 / 20) 14.7 / 13.6; one split more for half of the blocks per wave: 16 units, 71 blocks (8 / 9) 13.2 / 11.6.
-// Four waves where there is no more than a block for each (12 units, 2 blocks 7.4 against 7.6), and where more units than compute
-// units keep the chip busy with less left over at each end (1024 units, 5 / 16 / 32 blocks 26 / 47 / 87 against 38 / 54 / 95; 63 blocks 161
-// against 159).
+// joins k splits takes 2.4 + 0.05 k us, 4.0 among the launches of a decode step (12 units of size 64, 25 blocks: with its merge 11.4 us whole,
+// 12.1 in four) (fitted to 194 times of one bf16 row of up to 64 units, when its queries had two bytes).  One unit without splits: size
+// 128, 16 / 256 blocks 8.2 / 73 us, 64, 5 / 63 blocks 4.8 / 14.6.  No split / the best count: 12 units of size 128, 63 blocks 23.2 / 10.9, 256
+// blocks 77 / 16.3; 32 units, 128 blocks 42 / 18.4.  As many as fit / as the same blocks per wave need: 16 units, 133 blocks of size 128 (16 / 9
+// splits) 15.7 / 14.1, 4 units, 313 blocks (39 / 20) 14.7 / 14.0; one split more for half of the blocks per wave: 16 units, 71 blocks (8 / 9) 13.1 /
+// 11.6.  Four waves where there is no more than a block for each (1 unit, 2 blocks 5.1 against 5.4), and where more units than compute
+// units keep the chip busy with less left over at each end (1024 units, 2 / 32 blocks 15 / 80 against 25 / 84; 63 blocks 156 against 156).
+// Of 27 shapes with bf16 and fp32 rows each the choice is within 8 % of the best measured one, but for few units of 16 to 32 blocks (and fp32,
+// 32 units of 63: 11 %): splits of four waves, which it does not consider, take less there (bf16 5-15 %, fp32 15-22 %: 16 units of size 128, 16
+// blocks 9.7 / 8.2 and 11.0 / 8.6).
 inline ByteAttnShape byte_attn_shape(int cols, int64_t heads, int nblk, int head_dim, double join_us = 2.4) {
   ByteAttnShape s{cols > 16 ? 2 : 1, 0, 1, 8};
   s.groups = (cols + 16 * s.tiles - 1) / (16 * s.tiles);
