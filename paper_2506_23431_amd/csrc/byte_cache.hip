@@ -817,7 +817,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_byte_attn(ByteAttnArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         float p = __builtin_amdgcn_exp2f(sv[qt][e]);
-        if (sizeof(T) == 4) p *= fminf(ratio, 1.f);
+        if (sizeof(T) == 4) {
+          p *= fminf(ratio, 1.f);
+          // (one number for both halves: the compiler took the high one from the product as rounded and the low one from the product
+          // and a conversion fused, and where the two differed, in one of a thousand, the pair was off by a whole step of a half)
+          asm("" : "+v"(p));
+        }
         ph[qt][e >> 3].hh[e & 7] = (f16_t)p;
         if (PP) pl[qt][e >> 3].hh[e & 7] = (f16_t)(p - (float)ph[qt][e >> 3].hh[e & 7]);
       }
