@@ -382,7 +382,7 @@ __device__ __forceinline__ intx4 mfma_codes(uint4 a, uint4 b, intx4 c) {
 // Measured: 32 requests, 4 query heads to each of 8 key heads, up to 8192 tokens of size 128 70 us, 4.9 TB/s (half queries); 16 rows of
 // 4 x 32 heads, up to 5000 tokens 25 us and 4.1 for the merge (bf16).  Few short heads are a chain of trips to memory: 12 heads of
 // 64, 1000 tokens 7 us, of which an empty launch is 2.3.  Pieces of a prompt are bound by what a SIMD issues: fp32, 2048 rows of 16 heads
-// of 128 over 6144 tokens 183 us, 470 TFLOP/s.
+// of 128 over 6144 tokens 177 us, 485 TFLOP/s.
 // PP: probabilities as pairs of halves (22 bits): fp32 outputs need them, and half outputs are rounded as finely as single
 // probabilities would be (error of the whole 1.3 times the output's rounding without).
 // CTX: the columns are a decode step's rows, which see the context up to their limit and generated tokens by their tags.  32 tokens
