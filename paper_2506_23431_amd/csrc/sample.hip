@@ -25,10 +25,11 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 
-// 2^y by n = the nearest whole number and the series of 2^f for f = y - n, |f| <= 1/2: the first term left out is below
-// (ln 2 / 2)^11 / 11! = 2.2e-13.  y <= 0 or NaN; from -1023 on down, and for NaN, it is zero (so a product that is fused into the
-// difference stays near n).  The nearest whole number is what adding 1.5 * 2^52 leaves in the last bits, and 2^n is its exponent's bits.
-__device__ __forceinline__ double exp2_64(double y) {
+// 2^(y + up) by n = the nearest whole number and the series of 2^f for f = y - n, |f| <= 1/2: the first term left out is below
+// (ln 2 / 2)^11 / 11! = 2.2e-13.  y <= 0 or NaN; from -1023 on down, and for NaN, it is at most 2^(up - 1022), zero for up = 0 (so a
+// product that is fused into the difference stays near n).  The nearest whole number is what adding 1.5 * 2^52 leaves in the last bits, and
+// 2^n is its exponent's bits; up_bits: (up + 1023) * 2^20.
+__device__ __forceinline__ double exp2_64(double y, uint32_t up_bits = 1023u << 20) {
   constexpr double WHOLE = 6755399441055744.0;
   y = fmax(y, -1023.0);
   const double t = y + WHOLE, f = y - (t - WHOLE);
@@ -37,8 +38,8 @@ __device__ __forceinline__ double exp2_64(double y) {
   double p = L10;
   p = fma(p, f, L9); p = fma(p, f, L8); p = fma(p, f, L7); p = fma(p, f, L6); p = fma(p, f, L5);
   p = fma(p, f, L4); p = fma(p, f, L3); p = fma(p, f, L2); p = fma(p, f, L); p = fma(p, f, 1.0);
-  const uint32_t n = (uint32_t)__double_as_longlong(t) + 1023u;
-  return p * __longlong_as_double((long long)((uint64_t)(n << 20) << 32));
+  const uint32_t n = ((uint32_t)__double_as_longlong(t) << 20) + up_bits;
+  return p * __longlong_as_double((long long)((uint64_t)n << 32));
 }
 
 // A row's values in granules of 16 bytes.  KB: kilobytes of LDS in which they are kept, KB / 16 granules of every thread, next to each
@@ -410,11 +411,20 @@ __global__ __launch_bounds__(1024) void k_sample(SampleArgs a) {
     if (tid < n) sm.sorted[at] = me;
     __syncthreads();
   };
-  // e in whole numbers of which one token has at most 2^51, and all together less than 2^63
-  const double unit = __longlong_as_double((long long)(1023 + min(51, 62 - (32 - __clz(V)))) << 52),
-               per_unit = __longlong_as_double((long long)(1023 - min(51, 62 - (32 - __clz(V)))) << 52);
   const float range = fminf(48.6f * t, top - low), per = range > 0.f && range < INFINITY ? BINS / range : 0.f;
   auto bin_of = [&](float x) { return min((int)((top - x) * per), BINS - 1); };
+  // e in whole numbers of which one token has at most 2^51 (and what roundings of its piece leave above), and all together less than 2^63: times
+  // 2^(bits + k), where the tokens of a piece are below 2^-k.  So a token is off by 2^-(bits + 1) of about itself, 2^-42 for the largest
+  // vocabulary, however many there are and all of them to the same side.  (Of one unit for all pieces, 2^-bits: 700 tokens off, with 2^20 alike at
+  // 2.8e-10 of the first.)
+  const int bits = min(51, 62 - (32 - __clz(V)));
+  const uint32_t fall = per > 0.f && per < INFINITY ? (uint32_t)(range * (float)c * (1048576.f / BINS)) : 0;     // (35900 at most)
+  const uint32_t scale0 = (uint32_t)(bits + 1023) << 20;
+  auto scale_of = [&](int b) { return (scale0 + __umul24(b, fall)) & 0xfff00000u; };                         // bits + k, as an exponent's bits
+  auto pow2 = [](int n) { return __longlong_as_double((long long)(1023 + n) << 52); };
+  // (added to 2^52, a number below it leaves itself, rounded, in the last bits)
+  auto whole = [](double x) { return (unsigned long long)(__double_as_longlong(x + 4503599627370496.0) & 0xfffffffffffffll); };
+  auto unit_of = [&](int b) { return pow2(1023 - (int)(scale_of(b) >> 20)); };
 
   // Moves the cut: by number (the first `most` of the tokens, MASS false) or by sum (those in front of which less than P of the sum of
   // the kept ones has gone by).  True: the tokens that are left, and perhaps some behind them, are sm.near_[0 .. *n_sorted), in no order, within the pieces in front of *deep.
@@ -430,14 +440,14 @@ __global__ __launch_bounds__(1024) void k_sample(SampleArgs a) {
       if (tid == 0) { sm.n_near = 0; sm.key_low = 0xffffffffu; sm.key_high = 0; sm.bin = -1; }
       __syncthreads();
       // (what is far below the largest lies in the last piece, most of the row where the temperature is low, and 64 lanes that add to one
-      // place take turns: there every thread counts by itself, and zeros, as the sums are, go to a place of each lane's)
+      // place take turns: there every thread counts by itself, and e that count as zero go to a place of each lane's)
       uint32_t n_last = 0;
       const float far = top - 48.6f * t;                   // (2^-70 and less of the largest)
       auto add = [&](float x, int b, bool counts) {
         if (MASS) {
-          // (added to 2^52, a number below it leaves itself, rounded, in the last bits)
-          const double y = fma(counts ? e_of(x) : 0.0, unit, 4503599627370496.0);
-          atomicAdd(&sm.mass[x >= far ? b : lane], (unsigned long long)(__double_as_longlong(y) & 0xfffffffffffffll));
+          const float z = counts ? x : -INFINITY;
+          const int at = level || z >= far ? b : lane;     // (of the first places' units what is far below the largest is zero)
+          atomicAdd(&sm.mass[at], whole(exp2_64(((double)z - mx) * c, scale_of(level ? bin : at))));
         } else if (counts) {
           if (b == BINS - 1) ++n_last;
           else atomicAdd(&sm.count[b], 1u);
@@ -483,8 +493,19 @@ __global__ __launch_bounds__(1024) void k_sample(SampleArgs a) {
         if (b0 < goal && b1 >= goal) { sm.bin = 2 * tid; sm.before = b0; sm.found = c0; }
         if (b1 < goal && upto >= goal) { sm.bin = 2 * tid + 1; sm.before = b1; sm.found = c1; }
       } else {
-        const unsigned long long m0 = sm.mass[2 * tid], m1 = sm.mass[2 * tid + 1];
-        unsigned long long upto = wave_running(m0 + m1), all = 0;
+        unsigned long long m0 = sm.mass[2 * tid], m1 = sm.mass[2 * tid + 1], all = 0;
+        double per_unit = unit_of(max(bin, 0));
+        if (level == 0) {                                  // in one unit, by what they come to: about 2^-50 of that
+          const double d0 = (double)m0 * unit_of(2 * tid), d1 = (double)m1 * unit_of(2 * tid + 1);
+          const float mine = fold_wave((float)(d0 + d1), Add());
+          if (lane == 0) sm.top[wave] = mine;
+          __syncthreads();
+          const uint32_t sum = __builtin_amdgcn_readfirstlane(__float_as_uint(fold_row(sm.top[lane & 15], Add())));
+          const int up = 50 + 127 - (int)(sum >> 23);     // (in which the sum is below 2^52)
+          m0 = whole(d0 * pow2(up)); m1 = whole(d1 * pow2(up));
+          per_unit = pow2(-up);
+        }
+        unsigned long long upto = wave_running(m0 + m1);
         if (lane == 63) sm.wave_mass[wave] = upto;
         __syncthreads();
 #pragma unroll
