@@ -530,7 +530,7 @@ typedef struct {
 
 /* One token per row.
  *   logits     [n_row][vocab] of one of the PD_TYPE_* types, row r at logits + r * row_stride elements; vocab at most PD_SAMPLE_VOCAB
- *   u          fp32 [n_row], random numbers within [0, 1); others count as the nearest of these
+ *   u          fp32 [n_row], random numbers within [0, 1); others count as the nearest of these, 1 - 2^-24 above, NaN as 0
  *   params     HOST
  *   out_token  int32 [n_row];  out_logprob  fp32 [n_row] or NULL: log of the token's e over the total of those that stay (0 for token -1)
  * All in 64 bits: which token a number falls on is that of the formulas but for numbers within about 1e-10 of a border.  The same inputs

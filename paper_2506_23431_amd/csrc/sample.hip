@@ -211,7 +211,7 @@ __global__ __launch_bounds__(1024) void k_sample(SampleArgs a) {
   const float t = a.p.row_temperature ? a.p.row_temperature[r] : a.p.temperature;
   const float P = a.p.row_top_p ? a.p.row_top_p[r] : a.p.top_p, M = a.p.row_min_p ? a.p.row_min_p[r] : a.p.min_p;
   const int K = a.p.row_top_k ? a.p.row_top_k[r] : a.p.top_k;
-  const float u = a.u[r];
+  const float u = fminf(fmaxf(a.u[r], 0.f), 0x1.fffffep-1f);       // (within [0, 1); NaN is 0)
 
   // ---- the largest and the smallest value ----
   top = fold_wave(top, Max());
@@ -637,7 +637,7 @@ __global__ __launch_bounds__(1024) void k_sample(SampleArgs a) {
       ordered(by_index, n);
       const unsigned long long by = lane < n ? sm.sorted[n - 1 - lane] : 0;
       e = lane < n ? sm.weight[(uint32_t)by] : 0.0;
-      const double passed = wave_running(e), total = from_lane(passed, 63), target = u > 0.f ? (double)u * total : 0.0;
+      const double passed = wave_running(e), total = from_lane(passed, 63), target = (double)u * total;
       const uint64_t hit = __ballot(lane < n && (passed > target || lane == n - 1));
       if (lane == __ffsll((unsigned long long)hit) - 1) {
         a.token[r] = (int)(by >> 32);
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(1024) void k_sample(SampleArgs a) {
     const unsigned long long by = tid < n ? sm.sorted[n - 1 - tid] : 0;
     e = tid < n ? sm.weight[(uint32_t)by] : 0.0;
     double total;
-    const double passed = running(e, &total), target = u > 0.f ? (double)u * total : 0.0;
+    const double passed = running(e, &total), target = (double)u * total;
     // (the last one where rounding leaves none)
     const int first = first_thread(tid < n && (passed > target || tid == n - 1));
     if (tid == first) {
@@ -677,7 +677,7 @@ __global__ __launch_bounds__(1024) void k_sample(SampleArgs a) {
   if (P < 1.f) move_cut(std::true_type(), 0, nullptr, nullptr);
 
   // ---- the draw ----
-  auto goal = [&](double all) { return u > 0.f ? (double)u * all : 0.0; };
+  auto goal = [&](double all) { return (double)u * all; };
   const double least = M;
   Found f;
   if (cut == -INFINITY && !(M > 0.f)) f = locate([&](float x, int) { return e_of(x); }, goal);

@@ -6,7 +6,10 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_sampling import DEV, TYPES
+from test_gpu_sampling import DEV, TYPES, stay
+
+LAST = 1 - 2.0 ** -24                                        # the largest fp32 number below 1
+
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
@@ -38,3 +41,30 @@ def test_many_tokens_alike(kind, vocab):
                 assert token.item() == 0
                 off = abs(-logprob.double().item() - want)
                 assert off <= 1e-10 + (tail[0] + 1e-13) / (1 + math.expm1(want)) + 2.0 ** -24 * want, (low, t, rank, len(values), part, off)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [900, 5000, 32000, 70001])
+def test_random_numbers_of_one_and_above_are_the_last_below(vocab):
+    """The last tokens hold less than 2^-24 of the sum: a number below 1 does not reach them."""
+    from paper_2506_23431_amd import sample
+    g = torch.Generator(device=DEV)
+    g.manual_seed(vocab)
+    x = torch.randn(3, vocab, generator=g, device=DEV)
+    x[:, -vocab // 3:] -= 40.0
+    last = torch.full((3,), LAST, device=DEV)
+    for more in (dict(), dict(top_p=0.9999999), dict(min_p=1e-30), dict(top_k=vocab * 2 // 3 + 20), dict(top_k=vocab * 2 // 3 + 20, top_p=0.9999999)):
+        want = sample(x, last, with_logprob=True, **more)
+        if "top_p" not in more:
+            rows = [stay(r.double().cpu().numpy(), 1.0, more.get("top_k", 0), 1.0, more.get("min_p", 0.0)) for r in x]
+            assert want[0].tolist() == [idx[np.searchsorted(np.cumsum(e) / e.sum(), LAST, side="right")] for idx, e in rows]
+        for bad in (1.0, 1.5, 3e38, math.inf):
+            got = sample(x, torch.full((3,), bad, device=DEV), with_logprob=True, **more)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (more, bad)
+    # few by rank: one wave puts them in order; and more, all threads
+    for few in (50, 400):
+        y = x.clone()
+        y[:, -few // 2:] = -30.0
+        y[:, few // 2:-few // 2] = -60.0
+        got = [sample(y, torch.full((3,), v, device=DEV), top_k=few) for v in (LAST, 1.0, math.inf)]
+        assert (got[0] < few // 2).all() and torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
