@@ -1,4 +1,5 @@
-"""The choice of tokens next to its borders, against the definition in 64-bit numpy."""
+"""The choice of tokens next to its borders: sums over many tokens that are alike, rows whose tokens crowd where a cut lies, random
+numbers outside [0, 1), the largest vocabulary.  Against the definition in 64-bit numpy."""
 
 import math
 
@@ -41,6 +42,98 @@ def test_many_tokens_alike(kind, vocab):
                 assert token.item() == 0
                 off = abs(-logprob.double().item() - want)
                 assert off <= 1e-10 + (tail[0] + 1e-13) / (1 + math.expm1(want)) + 2.0 ** -24 * want, (low, t, rank, len(values), part, off)
+
+
+def between(e, rng):
+    """A random number (fp32) in the middle of a token of a random place, and the place; its rounding is at most 2^-25."""
+    share = e / e.sum()
+    at = rng.choice(np.flatnonzero(share > 2.0 ** -22))
+    return np.float32(np.cumsum(share)[at] - share[at] / 2), at
+
+
+def compare(x, cases, seed):
+    """Every case of (temperature, top_k, top_p, min_p) on the one row x: the token, and by the logarithm of its probability how many stay."""
+    from paper_2506_23431_amd import sample
+    rng = np.random.default_rng(seed)
+    row = x[0].double().cpu().numpy()
+    for case in cases:
+        idx, e = stay(row, *case)
+        u, at = between(e, rng)
+        want = math.log(e[at] / e.sum())
+        token, logprob = sample(x, torch.tensor([u], device=DEV), temperature=case[0], top_k=case[1], top_p=case[2], min_p=case[3], with_logprob=True)
+        assert token.item() == idx[at], case
+        assert abs(logprob.double().item() - want) <= 2.0 ** -24 * abs(want) + 1e-9, case
+
+
+def crowded(vocab, kind, seed):
+    """A token far above the others, one far below, and all others within a small part of the range between: a third of them by
+    octaves around zero, a third within 2^-10 of a value, a third within some 200 of the type's steps of another."""
+    rng = np.random.default_rng(seed)
+    n = vocab - 2
+    x = np.concatenate([rng.choice([-1.0, 1.0], n // 3) * 2.0 ** rng.uniform(-22, -8, n // 3), 0.0037 * (1 + rng.uniform(0, 2.0 ** -10, n // 3)),
+                        np.float32(0.0027) + rng.integers(0, 200, n - n // 3 * 2) * 2.0 ** -32, [40.0, -30.0]])
+    rng.shuffle(x)
+    return torch.tensor(x, dtype=torch.float32).to(TYPES[kind])[None]
+
+
+def keys(x):
+    """The order of fp32 numbers as whole ones."""
+    b = (x.astype(np.float32) + np.float32(0)).view(np.uint32).astype(np.int64)
+    return np.where(b >> 31, 0xffffffff - b, b | 0x80000000)
+
+
+def refinements(x, t, most):
+    """How often the range is cut anew for the `most` first of x, as the kernel does: 2048 pieces of the range, then of the keys in the piece with
+    the cut, as long as more than 1024 tokens of different values lie in it."""
+    top = x.max()
+    piece = np.minimum((top - x) / min(48.6 * t, top - x.min()) * 2048, 2047).astype(int)
+    inside, k, number = x, keys(x), 0
+    while True:
+        ends = np.cumsum(np.bincount(piece, minlength=2048))
+        b = int(np.searchsorted(ends, most))
+        most -= int(ends[b - 1]) if b else 0
+        k = k[piece == b]
+        if len(k) <= 1024 or k.min() == k.max():
+            return number
+        number += 1
+        piece = (k.max() - k) >> max(int(k.max() - k.min()).bit_length() - 11, 0)
+
+
+RANKS = (0.05, 0.2, 0.35, 0.5, 0.63, 0.8, 0.97)
+
+
+@pytest.mark.parametrize("vocab", [12000, 70001, 160000])
+def test_crowded_rows_need_one_two_and_three_cuts(vocab):
+    x = crowded(vocab, "f32", vocab)[0].numpy()
+    found = {refinements(x, 10.0, int(part * vocab)) for part in RANKS}
+    assert found >= {1, 3} and (vocab == 160000 or 2 in found)
+    for kind in ("bf16", "f16"):
+        y = crowded(vocab, kind, vocab)[0].float().numpy()
+        assert max(refinements(y, 10.0, int(part * vocab)) for part in RANKS) >= 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [12000, 32000, 50265, 70001, 160000])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_cuts_where_tokens_crowd(vocab, kind):
+    x = crowded(vocab, kind, vocab).to(DEV)
+    by_rank = [(10.0, int(part * vocab), 1.0, 0.0) for part in RANKS]
+    by_mass = [(10.0, 0, part, 0.0) for part in RANKS]
+    both = [(10.0, int(part * vocab), 0.5 + part / 3, 0.0) for part in RANKS]
+    compare(x, by_rank + by_mass + both + [(10.0, vocab // 2, 0.9, 0.01), (30.0, 0, 0.6, 0.0)], seed=vocab)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_the_largest_vocabulary(kind):
+    vocab = 1 << 20
+    g = torch.Generator(device=DEV)
+    g.manual_seed(9)
+    x = torch.randn(2, vocab + 1, generator=g, device=DEV) * 2
+    x[:, ::1001] += 6
+    x = x.to(TYPES[kind])[1:, 1:]                            # (begins beside a multiple of 16 bytes)
+    compare(x, [(1.0, 0, 1.0, 0.0), (0.8, 0, 0.9, 0.0), (0.7, 50, 0.95, 0.01), (1.0, 300000, 1.0, 0.0), (1.0, 300000, 0.7, 0.0), (0.6, 0, 1.0, 0.05)], seed=1)
+    compare(crowded(vocab, kind, 5).to(DEV), [(10.0, 700000, 1.0, 0.0), (10.0, 0, 0.55, 0.0), (10.0, 900000, 0.8, 0.0)], seed=2)
 
 
 @pytest.mark.gpu
