@@ -480,18 +480,25 @@ inline PageAttnShape page_attn_shape(int kv_heads, int n_req, int n_group, int c
       return s;
     }
   }
-  // Nothing shared and few columns: as many splits as cost least, where a second launch takes 3.8 us and 0.05 for each, and memory is the
-  // floor of all (heads of 64, 12 units, 16 / 32 blocks, one launch / two 6.9 / 8.4 and 9.4 / 7.8; of 128, 128 units, 24 / 47 blocks 19.5 / 23.7
-  // and 32.5 / 36.9).
+  // Nothing shared and few columns: as many splits as cost least, on at most one work-group per compute unit (some with two take as long as all
+  // with two: 48 units, 250 blocks, heads of 64, 240 / 288 work-groups 41.6 / 50.4).  A work-group's four waves take a block each at a time, which
+  // from memory is on its way for 0.0188 us a dim (54 KB a us and work-group, heads of 128); all together get no more than memory has, and less
+  // than the slower of the two where they are alike; the second launch reads eight splits at a time.  us by splits, tokens that no cache
+  // holds, heads of 128: 8 units, 16 blocks, 1 / 4 / 8 15.2 / 11.2 / 10.1; 512 blocks, 8 / 16 / 32 / 64 52.7 / 35.9 / 33.8 / 36.6; 2048 179 / 110 / 101 / 103;
+  // 64 units, 128 blocks, 1 / 2 / 4 / 8 91.7 / 59.3 / 54.5 / 53.2; 128 units, 24 blocks, 1 / 2 25.6 / 25.6, 64 56.6 / 54.0; heads of 64, 12 units, 16 blocks,
+  // 1 / 8 9.5 / 9.2.  What a cache holds comes in half the time, so little is not worth it: 8 units, 11 blocks, 1 / 8 12.3 / 10.0, there 8.4 / 9.0; 128 units,
+  // 64 blocks, 1 / 2 there 42.7 / 49.0.
   if (o.width == 16 && !n_group) {
-    const int64_t most = std::min<int64_t>(512 / std::max<int64_t>(1, o.units), o.blocks / 4);
-    const double floor_us = 3 + (double)o.units * o.blocks * read / 5;
-    double least = std::max(chain(o.blocks), floor_us), last = 1e30;
-    for (int k = 2; k <= most; ++k) {
-      const double us = std::max(chain((double)o.blocks / k), floor_us) + 3.8 + 0.05 * k;
-      if (us >= last) break;                               // (it only rises from there on)
-      last = us;
-      if (us < least) { least = us; o.splits = k; }
+    const int quads = (o.blocks + 3) / 4, most = (int)std::min<int64_t>(256 / o.units, o.blocks);
+    const double memory = 3 + (double)o.units * o.blocks * read / 5.6;
+    auto us = [&](int k) {
+      const double walk = 4.5 + (quads + k - 1) / k * (0.0188 * head_dim), more = std::max(walk, memory), less = std::min(walk, memory);
+      return more + 0.26 * less * (less / more) * (less / more) + (k == 1 ? 0. : 2.4 + 0.1 * k + (k % 8 ? 1.2 : 0.));
+    };
+    double least = us(1) - std::max(1.7, 0.06 * us(1));
+    for (int k = 2; k <= most; k += k < 16 ? 1 : 8) {
+      const double t = us(k);
+      if (t < least) { least = t; o.splits = k; }
     }
     return s;
   }
