@@ -449,7 +449,8 @@ int pd_byte_context(pd_ctx *ctx, void *dev_buffer, size_t bytes, void *hip_strea
 
 /* ---- operators of continuations of one input: a cache in pages, attention over a shared prefix, choice of tokens --------------
  * As the operators above: independent of any pd_ctx, on the current device and `hip_stream`, no call synchronises, allocates or keeps
- * anything, all can be captured into a graph, and `lens`, `pages` and the other DEVICE numbers are read when the kernels run.
+ * anything, all can be captured into a graph, and `lens`, `pages` and the other DEVICE numbers are read when the kernels run.  Calls whose
+ * launch would have 2^32 threads or more are refused: 2^24 pages of 8 heads to store or read or pieces of attention, 2^22 rows to draw from.
  *
  * The cache.  Tokens lie in pages of PD_PAGE, each with the keys and values of every key head in one 16-bit type; token t of a request
  * lies in place t mod PD_PAGE of page pages[request][t / PD_PAGE].  Which pages are whose is the caller's to know: requests that

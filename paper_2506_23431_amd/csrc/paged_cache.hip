@@ -745,9 +745,11 @@ __global__ __launch_bounds__(256, 2) void k_page_attn(PageAttnArgs a) {
 // The partial results of a row and head become one: a lane has four dims of them, 8 to 32 lanes a row and head, and all of these look
 // at every part's maximum and sum themselves (a wave a row, with the parts' factors from lane to lane: 15 us for 5.8, 16384 rows of
 // 64 dims in three parts; 6.0 for 5.3, 1024 rows of 128 in 17).  Bound by the trips to memory: 4 to 7 us.
+constexpr int merge_lanes(int hd) { return hd == 96 ? 32 : hd / 4; }
+constexpr int merge_rows(int hd) { return 256 / merge_lanes(hd); }
 template <typename CT, int HD>
 __global__ __launch_bounds__(256) void k_page_merge(PageAttnArgs a) {
-  constexpr int LANES = HD == 96 ? 32 : HD / 4;
+  constexpr int LANES = merge_lanes(HD);
   const int d = threadIdx.x % LANES * 4;
   const int64_t rows = (int64_t)a.n_req * a.n_row * a.n_head, i = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   const bool there = i < rows, mine = there && d < HD;
@@ -818,8 +820,9 @@ static int check_type(int type) {
              "type must be PD_TYPE_F32, PD_TYPE_BF16 or PD_TYPE_F16 (got %d)", type);
   return PD_OK;
 }
-static int check_grid(int64_t blocks) {
-  PD_REQUIRE(blocks < (1ll << 31), PD_EINVAL, "a launch of %lld work-groups is too large", (long long)blocks);
+// a launch of a * b work-groups of 256 threads, of which it may have fewer than 2^32
+static int check_grid(int64_t a, int64_t b = 1) {
+  PD_REQUIRE(a < (1 << 24) && b < (1 << 24) && a * b < (1 << 24), PD_EINVAL, "a launch of %lld x %lld work-groups is too large", (long long)a, (long long)b);
   return PD_OK;
 }
 
@@ -873,8 +876,8 @@ extern "C" int pd_page_append(const pd_page_cache *cache, const int32_t *pages, 
     bits |= (uintptr_t)a.src[i] | (uint64_t)((st[0] | st[1] | st[2]) * es);
   }
   const bool wide = (bits & 15) == 0;
-  const int64_t blocks = (int64_t)n_req * a.span * (a.groups[0] + a.groups[1] + a.groups[2]);
-  if ((rc = check_grid(blocks))) return rc;
+  const int64_t pieces = (int64_t)n_req * a.span, groups = a.groups[0] + a.groups[1] + a.groups[2], blocks = pieces * groups;
+  if ((rc = check_grid(pieces, groups))) return rc;
   hipStream_t s = (hipStream_t)hip_stream;
 #define PD_STORE(T, CT, HDV)                                                                                       \
   do {                                                                                                             \
@@ -898,8 +901,8 @@ extern "C" int pd_page_read(const pd_page_cache *cache, const int32_t *pages, in
   PageReadArgs a;
   a.c = view(cache); a.out[0] = out_k; a.out[1] = out_v; a.first = first; a.lens = lens; a.pages = pages; a.n_tok = n_tok; a.n_slot = n_slot;
   a.span = (int)(first ? ((int64_t)n_tok - 1 + PD_PAGE - 1) / PD_PAGE + 1 : ((int64_t)n_tok + PD_PAGE - 1) / PD_PAGE);
-  const int64_t blocks = (int64_t)n_req * a.span * 2 * ((cache->n_kv_head + STORE_HEADS - 1) / STORE_HEADS);
-  if ((rc = check_grid(blocks))) return rc;
+  const int64_t pieces = (int64_t)n_req * a.span, groups = 2 * ((cache->n_kv_head + STORE_HEADS - 1) / STORE_HEADS), blocks = pieces * groups;
+  if ((rc = check_grid(pieces, groups))) return rc;
   hipStream_t s = (hipStream_t)hip_stream;
 #define PD_READ(T, CT, HDV) hipLaunchKernelGGL((k_page_read<T, CT, HDV>), dim3((unsigned)blocks), dim3(256), 0, s, a)
   PD_PAGE_TYPES(type, cache->type, cache->head_dim, PD_READ)
@@ -913,16 +916,18 @@ static int check_attention(const pd_page_cache *c, int n_req, int n_group, int n
   PD_REQUIRE(n_group >= 0 && (n_group == 0 || n_req % n_group == 0), PD_EINVAL, "%d requests do not form %d groups of one size", n_req, n_group);
   PD_REQUIRE(n_row >= 0 && max_shared >= 0 && max_behind >= 0, PD_EINVAL, "n_row, max_shared and max_behind must be >= 0 (got %d, %d, %d)",
              n_row, max_shared, max_behind);
-  PD_REQUIRE((int64_t)n_req * n_row * n_head < (1ll << 31), PD_EINVAL, "too many rows (%d x %d x %d)", n_req, n_row, n_head);
+  PD_REQUIRE((int64_t)n_row * n_head < (1ll << 31) && (int64_t)n_row * n_head * n_req < (1ll << 31), PD_EINVAL, "too many rows (%d x %d x %d)", n_req,
+             n_row, n_head);
   return PD_OK;
 }
 
-struct PageLaunch { PageWork part[2]; int64_t n_shared, n_own, n_cols; size_t bytes; };
+struct PageLaunch { PageWork part[2]; int64_t n_shared, n_own, n_cols, n_merge; size_t bytes; };
 
 static int page_launch(const pd_page_cache *c, int n_slot, int n_req, int n_group, int n_head, int n_row, int max_shared, int max_behind,
                        PageLaunch *out) {
   int rc = check_attention(c, n_req, n_group, n_head, n_row, max_shared, max_behind);
   if (rc) return rc;
+  if (n_row == 0) { *out = PageLaunch{}; return PD_OK; }
   const int cols = n_row * (n_head / c->n_kv_head);
   const PageAttnShape sh = page_attn_shape(c->n_kv_head, n_req, n_group, cols, n_slot, max_shared, max_behind, c->head_dim);
   for (int i = 0; i < 2; ++i) {
@@ -937,6 +942,8 @@ static int page_launch(const pd_page_cache *c, int n_slot, int n_req, int n_grou
   const bool alone = out->n_shared == 0 && sh.part[1].splits == 1;
   out->n_cols = alone ? 0 : page_columns(sh.part[0]) + page_columns(sh.part[1]);
   out->bytes = alone ? 16 : (size_t)out->n_cols * (c->head_dim + 2) * sizeof(float);
+  out->n_merge = alone ? 0 : ((int64_t)n_req * n_row * n_head + merge_rows(c->head_dim) - 1) / merge_rows(c->head_dim);
+  if ((rc = check_grid(out->n_merge))) return rc;
   return check_grid(out->n_shared + out->n_own);
 }
 
@@ -976,12 +983,11 @@ extern "C" int pd_page_attention(const pd_page_cache *cache, const int32_t *page
   a.q_wide = (((uintptr_t)q | (uint64_t)((q_strides[0] | q_strides[1] | q_strides[2]) * 2)) & 15) == 0;
   a.part[0] = l.part[0]; a.part[1] = l.part[1]; a.n_shared = l.n_shared; a.n_cols = l.n_cols; a.sums = (float *)workspace;
   hipStream_t s = (hipStream_t)hip_stream;
-  const unsigned grid = (unsigned)(l.n_shared + l.n_own), per = 256 / (cache->head_dim == 96 ? 32 : cache->head_dim / 4);
-  const unsigned rows = (unsigned)(((int64_t)n_req * n_row * n_head + per - 1) / per);
+  const unsigned grid = (unsigned)(l.n_shared + l.n_own), merge = (unsigned)l.n_merge;
 #define PD_ATTEND(CT, HDV)                                                                             \
   do {                                                                                                 \
     hipLaunchKernelGGL((k_page_attn<CT, HDV>), dim3(grid), dim3(256), 0, s, a);                        \
-    if (l.n_cols) hipLaunchKernelGGL((k_page_merge<CT, HDV>), dim3(rows), dim3(256), 0, s, a);         \
+    if (merge) hipLaunchKernelGGL((k_page_merge<CT, HDV>), dim3(merge), dim3(256), 0, s, a);          \
   } while (0)
   if (cache->type == PD_TYPE_BF16) PD_PAGE_DIMS(cache->head_dim, PD_ATTEND, bf16_t)
   else PD_PAGE_DIMS(cache->head_dim, PD_ATTEND, f16_t)

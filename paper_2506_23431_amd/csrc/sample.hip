@@ -706,6 +706,7 @@ template <typename T> static void run_sample(const SampleArgs &a, int n_row, hip
 }
 
 int launch_sample(const SampleArgs &a, int type, int n_row, hipStream_t s) {
+  PD_REQUIRE(n_row < (1 << 22), PD_EINVAL, "a launch of %d rows is too large", n_row);      // (of 1024 threads, of which it may have fewer than 2^32)
   if (type == PD_TYPE_F32) run_sample<float>(a, n_row, s);
   else if (type == PD_TYPE_BF16) run_sample<bf16_t>(a, n_row, s);
   else run_sample<f16_t>(a, n_row, s);
