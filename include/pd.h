@@ -509,7 +509,9 @@ int pd_page_read(const pd_page_cache *cache, const int32_t *pages, int n_slot, i
  *   workspace  at least pd_page_attention_workspace_bytes (same arguments; 0: they are invalid), 16-byte aligned; it holds nothing
  *              between calls, and calls that may overlap need one each
  * Scores, the running maximum and all sums are fp32; probabilities are rounded to the cache's type where they meet the values (2^-8 of
- * each at most, 2^-11 for halves), not where they are added up.  Infinities and NaN in tokens that a row does not see do not reach it. */
+ * each at most; 2^-11 for halves, or 2^-33 of the row's largest where that is more), not where they are added up.  Infinities and NaN
+ * in tokens that a row does not see do not reach it; but a row whose blocks of 64 hold such values goes a slow way, so pages are best zeroed before
+ * their first use. */
 size_t pd_page_attention_workspace_bytes(const pd_page_cache *cache, int n_slot, int n_req, int n_group, int n_head, int n_row,
                                          int max_shared, int max_behind);
 int pd_page_attention(const pd_page_cache *cache, const int32_t *pages, int n_slot, int n_req, const void *q,
