@@ -4,14 +4,14 @@
 // that order: the first k; those in front of which less than p of the sum of what k keeps has gone by; those with e_i >= min_p.  So a
 // row is cut at one place of the order, (value, index), and what is kept is drawn from in the order of the indices: nothing is sorted but
 // the few tokens around a cut.  A cut is found by histograms of numbers and sums of e over 2048 pieces of the range, in whole numbers of
-// 64 bits, which come out the same in whatever order they are added.
+// 64 bits of a unit for each piece, which come out the same in whatever order they are added.
 // Which token a number falls on depends on sums next to borders: e and all sums have 64 bits (a multiply-add of 64 bits takes this
 // chip 8 clocks a wave, twice one of 32).
 //
-// Bound by what one compute unit issues: a row is one work-group's.  Of the 25 us of a row of 32000 by top-p, loading and its largest
-// value take 3, e with its additions in LDS 7 (18 instructions of 64 bits, and 34 clocks for 64 additions to random places), what lies around
+// Bound by what one compute unit issues: a row is one work-group's.  Of the 26 us of a row of 32000 by top-p, loading and its largest
+// value take 3, e with its additions in LDS 8 (18 instructions of 64 bits, and 34 clocks for 64 additions to random places), what lies around
 // the cut 4, e once more and the running sums 8.  By rank nothing needs e but the few that stay: 13.9 us.  512 rows of 32128 by top-p (two
-// rounds of the 256 compute units) 58 us, 64 rows of 50265 46.
+// rounds of the 256 compute units) 60 us, 64 rows of 50265 47.  fp32 rows of 50265, which are read again in every pass, 48 us, of 128000 105.
 #include "pd_internal.h"
 
 #include <type_traits>
